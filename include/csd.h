@@ -37,7 +37,8 @@ typedef enum {
     CSD_ERR_CUDA = 5,        /* a CUDA runtime call failed (see csd_last_cuda_error)            */
     CSD_ERR_BAD_TOKEN = 6,   /* device status: a token id was outside [0, vocab)                */
     CSD_ERR_TIMEOUT = 7,     /* device status: a bounded probe loop reached its limit           */
-    CSD_ERR_UNSUPPORTED = 8
+    CSD_ERR_UNSUPPORTED = 8,
+    CSD_ERR_BAD_PAGE = 9     /* device status: a page id was outside [0, n_pages)               */
 } csd_status;
 
 const char* csd_status_string(csd_status s);
@@ -256,6 +257,94 @@ csd_status csd_spec_accept_static(const float* target_logits_dev, const float* d
                                   const int32_t* onehot_dev, const int32_t* draft_tokens_dev, int rows, int k, int V,
                                   float temperature, float lenience, uint64_t seed, uint64_t step,
                                   int32_t* n_accepted_dev, int32_t* out_token_dev, void* stream);
+
+/* The review rule on laws that are given as probabilities, with given random numbers: what a caller needs whose
+ * laws are no longer softmax(logits / T) (cut to their likeliest entries, mixed, or made elsewhere) or whose
+ * random numbers come from its own generator.  Row s has n_drafts_dev[s] drafts (0 .. k; NULL: k each) with
+ * target laws p_0 .. p_n and draft laws q_0 .. q_{n-1}; what lies behind them is not read.  x_i is accepted iff
+ * u_i * q_i(x_i) < p_i(x_i); at the first rejection i the output token is drawn from max(0, p_i - q_i) (from p_i
+ * where that carries nothing), if all n are accepted from p_n.  draft_probs_dev NULL: point masses, q_i(x_i) = 1 and
+ * 0 elsewhere.  The draw is the inverse CDF in vocabulary order, smallest j with cumulative mass > u_k * total, in fp64
+ * on the differences of the given numbers; laws need not sum to 1.  Entries that are not positive finite numbers carry
+ * no mass.  A law without any gives token 0.
+ *   target_probs_dev [rows, k+1, V], draft_probs_dev [rows, k, V] of prob_type (csd_row_type), consecutive laws ld_p and ld_q
+ *   entries apart (>= V); draft_tokens_dev [rows, k] int32 (0 <= k <= 64); uniforms_dev [rows, k+1] fp32 in [0, 1): one a draft,
+ *   the last for the output token.  Outputs: n_accepted_dev [rows]; tokens_dev [rows, k+1]: the accepted drafts, the output
+ *   token, and -1 behind it.
+ * A token id outside [0, V) is rejected and sets the device status to CSD_ERR_BAD_TOKEN, a count outside [0, k] is taken as
+ * the nearer end and sets CSD_ERR_INVALID_ARG, as does a number u outside [0, 1) (taken as the nearer end, NaN as 0). */
+typedef enum { CSD_F32 = 0, CSD_BF16 = 1 } csd_row_type;
+csd_status csd_spec_verify(const void* target_probs_dev, int64_t ld_p, const void* draft_probs_dev, int64_t ld_q, int prob_type,
+                           const int32_t* draft_tokens_dev, const int32_t* n_drafts_dev, const float* uniforms_dev, int rows,
+                           int k, int V, int32_t* n_accepted_dev, int32_t* tokens_dev, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Paged cache: the keys and values of many sequences in one pool of pages, for servers that review
+ * the blocks of several sequences together (not in the paper).  A page holds page_size consecutive
+ * positions of all heads, [kv head][slot][d_head]; a sequence is a row of the page table: position
+ * t lies in slot t % page_size of page page_table[s][t / page_size].
+ *   CSD_KV_BF16  rows rounded to bf16 (nearest-even)
+ *   CSD_KV_E4M3  a row of one position and head is d_head e4m3 numbers and one byte e + 127: the
+ *                values are the numbers times 2^e, e the smallest whole number, at least -100, with
+ *                max|x| <= 448 * 2^e over the row's finite entries (a power of two: scaling rounds
+ *                nothing, and a stored value is exact in fp32 and bf16).  Infinities become
+ *                +-448 * 2^e, NaN stays NaN; at e = 120 the
+ *                numbers end at 240 (256 * 2^120 is none in fp32).
+ * A batch is a chunk of new rows for each sequence: rows row_start[s] .. row_start[s+1] - 1 of the
+ * packed row arrays are sequence s at positions kv_len[s] .., kv_len[s] positions lie before them.
+ * The arrays are on the device, so a captured call replays with other lengths.  Lengths of zero are
+ * fine; rows of the arrays that belong to no sequence are left as they were.
+ * Found on the device: a page id outside [0, n_pages) sets CSD_ERR_BAD_PAGE (its positions are not
+ * written, read back as zeros, and seen by no row); a chunk that reaches behind max_pages pages sets
+ * CSD_ERR_CAPACITY (those positions likewise); counts outside their range (kv_len < 0, more than max_rows
+ * rows, rows behind total_rows) are cut to it and set CSD_ERR_INVALID_ARG.  Only pages that hold positions of the
+ * sequence are looked up.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { CSD_KV_BF16 = 0, CSD_KV_E4M3 = 1 } csd_kv_kind;
+typedef struct {
+    int32_t kind;         /* csd_kv_kind                                              */
+    int32_t n_pages;      /* n_pages * n_kv_heads * page_size < 2^31                  */
+    int32_t page_size;    /* 16, 32, 64 or 128 positions                              */
+    int32_t n_kv_heads;
+    int32_t d_head;       /* 64 or 128                                                */
+    void* k_dev;          /* [n_pages][n_kv_heads][page_size][d_head], 16-byte aligned */
+    void* v_dev;
+    uint8_t* k_exp_dev;   /* CSD_KV_E4M3: [n_pages][n_kv_heads][page_size], else NULL */
+    uint8_t* v_exp_dev;
+} csd_kv_pool;
+
+#define CSD_MAX_SEQS 1024
+typedef struct {
+    int32_t n_seqs;       /* 1 .. CSD_MAX_SEQS                                        */
+    int32_t max_pages;    /* columns of the page table; max_pages * page_size < 2^30  */
+    int32_t total_rows;   /* rows of the packed row arrays                            */
+    int32_t max_rows;     /* most rows of one sequence                                */
+    const int32_t* page_table_dev;   /* [n_seqs][max_pages]                           */
+    const int32_t* row_start_dev;    /* [n_seqs + 1], not decreasing                  */
+    const int32_t* kv_len_dev;       /* [n_seqs]                                      */
+} csd_paged_batch;
+
+/* Writes the batch's rows to their positions.  k_dev and v_dev are [total_rows, n_kv_heads * d_head] of row_type, rows ld elements
+ * apart (a multiple of 8; 16-byte aligned). */
+csd_status csd_paged_append(const csd_kv_pool* pool, const csd_paged_batch* batch, const void* k_dev, const void* v_dev, int64_t ld,
+                            int row_type, void* stream);
+/* Reads the batch's positions back as the values they stand for (to bf16 rows: exactly, both kinds). */
+csd_status csd_paged_read(const csd_kv_pool* pool, const csd_paged_batch* batch, void* k_dev, void* v_dev, int64_t ld, int row_type,
+                          void* stream);
+
+/* Attention of the batch's rows over the cache that already holds their keys (csd_paged_append first):
+ * out_r = sum_j softmax_j(scale * q_r . k_j) v_j over the positions j that the row sees: the kv_len before the chunk and,
+ * of the chunk itself, its rows up to its own or, with tree_mask_dev [total_rows], the rows whose bit is set (bit j: row j
+ * of the same sequence's chunk; max_rows <= 64).  A row that sees nothing is 0.  q_dev [total_rows, n_heads * d_head], rows ldq
+ * elements apart, out_dev likewise with ldo (multiples of 8; 16-byte aligned; out may not overlap q).  n_heads is a multiple of
+ * the pool's kv heads, at most 64 times as many; query head h reads kv head h / (n_heads / n_kv_heads).  Scores, softmax and sums are fp32; bf16 rows enter the products as they are
+ * and their weights as bf16, fp32 rows and weights as three bf16 terms each.
+ * The workspace has to be zero before its first call; every call leaves it ready for the next, of any shape.  Calls that may overlap
+ * on the GPU need workspaces of their own. */
+size_t csd_paged_attention_workspace_bytes(const csd_kv_pool* pool, const csd_paged_batch* batch, int n_heads, int row_type);
+csd_status csd_paged_attention(const csd_kv_pool* pool, const csd_paged_batch* batch, const void* q_dev, int64_t ldq, int n_heads,
+                               int row_type, float scale, const uint64_t* tree_mask_dev, void* out_dev, int64_t ldo,
+                               void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Max-Gram statistical drafter (Section 3.3, Appendix A): the longest suffix of the sequence

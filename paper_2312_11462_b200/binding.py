@@ -24,7 +24,8 @@ lib = C.CDLL(LIB_PATH)
 
 CSD_OK = 0
 STATUS_NAMES = {0: "CSD_OK", 1: "CSD_ERR_INVALID_ARG", 2: "CSD_ERR_SHAPE", 3: "CSD_ERR_CAPACITY", 4: "CSD_ERR_OOM",
-                5: "CSD_ERR_CUDA", 6: "CSD_ERR_BAD_TOKEN", 7: "CSD_ERR_TIMEOUT", 8: "CSD_ERR_UNSUPPORTED"}
+                5: "CSD_ERR_CUDA", 6: "CSD_ERR_BAD_TOKEN", 7: "CSD_ERR_TIMEOUT", 8: "CSD_ERR_UNSUPPORTED",
+                9: "CSD_ERR_BAD_PAGE"}
 
 
 class CsdError(RuntimeError):
@@ -63,7 +64,17 @@ class Profile(C.Structure):
                 ("other_launches", C.c_int64)]
 
 
-_vp, _i, _sz, _f, _u64 = C.c_void_p, C.c_int, C.c_size_t, C.c_float, C.c_uint64
+class KvPoolStruct(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("kind", "n_pages", "page_size", "n_kv_heads", "d_head")] + \
+               [(n, C.c_void_p) for n in ("k_dev", "v_dev", "k_exp_dev", "v_exp_dev")]
+
+
+class PagedBatchStruct(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "max_pages", "total_rows", "max_rows")] + \
+               [(n, C.c_void_p) for n in ("page_table_dev", "row_start_dev", "kv_len_dev")]
+
+
+_vp, _i, _sz, _f, _u64, _i64 = C.c_void_p, C.c_int, C.c_size_t, C.c_float, C.c_uint64, C.c_int64
 lib.csd_status_string.restype = C.c_char_p
 lib.csd_status_string.argtypes = [_i]
 lib.csd_last_cuda_error.restype = C.c_char_p
@@ -92,6 +103,12 @@ lib.csd_spec_accept_workspace_bytes.argtypes = [_i, _i, _i]
 lib.csd_spec_accept.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _f, _u64, _u64, _vp, _vp, _vp, _sz, _vp]
 lib.csd_spec_accept_static_capacity.restype = _sz
 lib.csd_spec_accept_static.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _f, _f, _u64, _u64, _vp, _vp, _vp]
+lib.csd_spec_verify.argtypes = [_vp, _i64, _vp, _i64, _i, _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp]
+lib.csd_paged_append.argtypes = [_vp, _vp, _vp, _vp, _i64, _i, _vp]
+lib.csd_paged_read.argtypes = [_vp, _vp, _vp, _vp, _i64, _i, _vp]
+lib.csd_paged_attention_workspace_bytes.restype = _sz
+lib.csd_paged_attention_workspace_bytes.argtypes = [_vp, _vp, _i, _i]
+lib.csd_paged_attention.argtypes = [_vp, _vp, _vp, _i64, _i, _i, _f, _vp, _vp, _i64, _vp, _sz, _vp]
 lib.csd_mag_workspace_bytes.restype = _sz
 lib.csd_mag_workspace_bytes.argtypes = [_i, _i, _i]
 lib.csd_mag_create.argtypes = [_vp, _i, _i, _vp, _i, _i, _vp, _sz, _vp, _vp]
@@ -311,6 +328,149 @@ def csd_spec_accept_static(target_logits: torch.Tensor, draft_logits: Optional[t
            lib.csd_spec_accept_static(_ptr(target_logits), _ptr(draft_logits), _ptr(onehot), _ptr(draft_tokens), rows,
                                       k1 - 1, V, temperature, lenience, seed, step, _ptr(out[0]), _ptr(out[1]),
                                       _stream()))
+    return out
+
+
+ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _on(device: torch.device):
+    """The device's current stream, and the device made current for the call where it is not."""
+    index = device.index
+    if index == torch.cuda.current_device():
+        return torch._C._cuda_getCurrentRawStream(index), None
+    return torch.cuda.current_stream(index).cuda_stream, torch.cuda.device(index)
+
+
+def _call(name: str, fn, device: torch.device, *args) -> None:
+    """fn(*args, stream) on the tensors' device."""
+    stream, guard = _on(device)
+    if guard is None:
+        code = fn(*args, stream)
+    else:
+        with guard:
+            code = fn(*args, stream)
+    if code:
+        raise CsdError(name, code)
+
+
+def csd_spec_verify(target_probs: torch.Tensor, draft_probs: Optional[torch.Tensor], draft_tokens: torch.Tensor,
+                    uniforms: torch.Tensor, n_drafts: Optional[torch.Tensor] = None, out: Optional[Sequence[torch.Tensor]] = None):
+    """The review rule on given probabilities with given random numbers.  target_probs [rows, k+1, V] and draft_probs
+    [rows, k, V] (None: point masses) float32 or bfloat16, uniforms [rows, k+1] float32, n_drafts [rows] int32 (None: k
+    each).  Laws may lie further apart than V (a view of a padded vocabulary).  Returns (n_accepted [rows], tokens
+    [rows, k+1]: the accepted drafts, the output token, -1 behind it), int32."""
+    rows, k1, V = target_probs.shape
+    k, dev = k1 - 1, target_probs.device
+    ld_p, ld_q = _law_stride(target_probs), 0
+    if draft_probs is not None:
+        assert draft_probs.dtype == target_probs.dtype and tuple(draft_probs.shape) == (rows, k, V) and draft_probs.device == dev
+        ld_q = _law_stride(draft_probs) if k else V
+    assert draft_tokens.dtype == torch.int32 and draft_tokens.is_contiguous() and tuple(draft_tokens.shape) == (rows, k)
+    assert uniforms.dtype == torch.float32 and uniforms.is_contiguous() and tuple(uniforms.shape) == (rows, k1)
+    assert n_drafts is None or (n_drafts.dtype == torch.int32 and n_drafts.is_contiguous() and n_drafts.numel() == rows)
+    if out is None:
+        out = (torch.empty(rows, dtype=torch.int32, device=dev), torch.empty(rows, k1, dtype=torch.int32, device=dev))
+    _call("csd_spec_verify", lib.csd_spec_verify, dev, target_probs.data_ptr(), ld_p, _ptr(draft_probs), ld_q, ROW_TYPES[target_probs.dtype],
+          draft_tokens.data_ptr(), _ptr(n_drafts), uniforms.data_ptr(), rows, k, V, out[0].data_ptr(), out[1].data_ptr())
+    return out
+
+
+def _law_stride(t: torch.Tensor) -> int:
+    """Entries between the laws of [rows, n, V]; the laws of all rows are evenly spaced."""
+    a, ld, one = t.stride()
+    assert t.is_cuda and one == 1 and (t.shape[0] == 1 or a == t.shape[1] * ld)
+    return ld
+
+
+class KvPool:
+    """A paged cache over the caller's tensors: k and v [n_pages, n_kv_heads, page_size, d_head], bfloat16, or
+    float8_e4m3fn with the exponents k_exp and v_exp [n_pages, n_kv_heads, page_size] uint8."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: Optional[torch.Tensor] = None, v_exp: Optional[torch.Tensor] = None):
+        n, H, P, D = k.shape
+        assert k.is_cuda and k.shape == v.shape and k.dtype == v.dtype and k.is_contiguous() and v.is_contiguous() and v.device == k.device
+        if k.dtype == torch.bfloat16:
+            assert k_exp is None and v_exp is None
+        else:
+            assert k.dtype == torch.float8_e4m3fn
+            for e in (k_exp, v_exp):
+                assert e.dtype == torch.uint8 and tuple(e.shape) == (n, H, P) and e.is_contiguous() and e.device == k.device
+        self.k, self.v, self.k_exp, self.v_exp, self.device, self.heads, self.d_head = k, v, k_exp, v_exp, k.device, H, D
+        self.c = KvPoolStruct(int(k.dtype != torch.bfloat16), n, P, H, D, _ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp))
+        self.ref = C.addressof(self.c)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, d_head: int, dtype: torch.dtype = torch.bfloat16, device="cuda"):
+        shape = (n_pages, n_kv_heads, page_size, d_head)
+        k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        if dtype == torch.bfloat16:
+            return cls(k, v)
+        return cls(k, v, *(torch.empty(shape[:3], dtype=torch.uint8, device=device) for _ in range(2)))
+
+
+class PagedBatch:
+    """The chunks of new rows of several sequences: page_table [n_seqs, max_pages], row_start [n_seqs + 1], kv_len [n_seqs]
+    (int32 on the GPU; their values may change between calls), rows of the packed row arrays, most rows of one sequence."""
+
+    def __init__(self, page_table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor, total_rows: int, max_rows: int):
+        n, pages = page_table.shape
+        for t in (page_table, row_start, kv_len):
+            assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.device == page_table.device
+        assert row_start.numel() == n + 1 and kv_len.numel() == n
+        self.page_table, self.row_start, self.kv_len, self.total_rows, self.max_rows = page_table, row_start, kv_len, total_rows, max_rows
+        self.c = PagedBatchStruct(n, pages, total_rows, max_rows, _ptr(page_table), _ptr(row_start), _ptr(kv_len))
+        self.ref = C.addressof(self.c)
+
+
+def _row_stride(t: torch.Tensor, batch: PagedBatch, heads: Optional[int], d_head: int, device: torch.device) -> int:
+    """Elements between the rows of [total_rows, heads, d_head], whose heads lie side by side."""
+    assert t.device == device and t.shape[0] == batch.total_rows and t.shape[2] == d_head and (heads is None or t.shape[1] == heads)
+    a, b, one = t.stride()
+    assert one == 1 and (t.shape[1] == 1 or b == d_head)
+    return a if t.shape[0] > 1 else t.shape[1] * d_head
+
+
+def csd_paged_append(pool: KvPool, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor) -> None:
+    """Writes rows k and v [total_rows, n_kv_heads, d_head] (float32 or bfloat16) to the batch's positions of the pool."""
+    ld = _row_stride(k, batch, pool.heads, pool.d_head, pool.device)
+    assert k.dtype == v.dtype and _row_stride(v, batch, pool.heads, pool.d_head, pool.device) == ld
+    _call("csd_paged_append", lib.csd_paged_append, pool.device, pool.ref, batch.ref, k.data_ptr(), v.data_ptr(), ld, ROW_TYPES[k.dtype])
+
+
+def csd_paged_read(pool: KvPool, batch: PagedBatch, dtype: torch.dtype = torch.bfloat16, out: Optional[Sequence[torch.Tensor]] = None):
+    """The values that the pool holds at the batch's positions: (k, v), each [total_rows, n_kv_heads, d_head]."""
+    if out is None:
+        out = tuple(torch.empty(batch.total_rows, pool.heads, pool.d_head, dtype=dtype, device=pool.device) for _ in range(2))
+    k, v = out
+    ld = _row_stride(k, batch, pool.heads, pool.d_head, pool.device)
+    assert k.dtype == v.dtype and _row_stride(v, batch, pool.heads, pool.d_head, pool.device) == ld
+    _call("csd_paged_read", lib.csd_paged_read, pool.device, pool.ref, batch.ref, k.data_ptr(), v.data_ptr(), ld, ROW_TYPES[k.dtype])
+    return out
+
+
+def csd_paged_attention_workspace(pool: KvPool, batch: PagedBatch, n_heads: int, dtype: torch.dtype) -> torch.Tensor:
+    return _ws(lib.csd_paged_attention_workspace_bytes(pool.ref, batch.ref, n_heads, ROW_TYPES[dtype]), pool.device)
+
+
+def csd_paged_attention(q: torch.Tensor, pool: KvPool, batch: PagedBatch, scale: Optional[float] = None,
+                        tree_mask: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of rows q [total_rows, n_heads, d_head] (float32 or bfloat16) over the pool, which holds the rows' own keys
+    already.  scale None: 1 / sqrt(d_head); tree_mask [total_rows] int64 (bit j: sees row j of its chunk) instead of causal.
+    A workspace is zero before its first call and not shared by calls that may overlap."""
+    heads, D = q.shape[1], pool.d_head
+    ldq = _row_stride(q, batch, None, D, pool.device)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert out.dtype == q.dtype and out.shape == q.shape
+    if workspace is None:
+        workspace = csd_paged_attention_workspace(pool, batch, heads, q.dtype)
+    if tree_mask is not None:
+        assert tree_mask.dtype == torch.int64 and tree_mask.is_contiguous() and tree_mask.numel() == batch.total_rows and tree_mask.device == q.device
+    _call("csd_paged_attention", lib.csd_paged_attention, pool.device, pool.ref, batch.ref, q.data_ptr(), ldq, heads, ROW_TYPES[q.dtype],
+          D ** -0.5 if scale is None else scale, _ptr(tree_mask), out.data_ptr(), _row_stride(out, batch, heads, D, pool.device),
+          workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return out
 
 

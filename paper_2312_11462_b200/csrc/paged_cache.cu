@@ -1,0 +1,205 @@
+// Writing rows into the paged cache, in 16 or 8 bits, and reading them back.
+//
+// A row of one position and head is quantised by the lanes that hold it: max|x| by a shuffle among them, the scale's exponent
+// from the maximum's bits (max|x| = m * 2^x with m in [1, 2): 448 = 1.75 * 2^8, so e = x - 8, one more where m > 1.75), then
+// rn_e4m3(x * 2^-e).  The scale is a power of two, so x * 2^-e is exact and the result does not depend on how it is formed.
+//
+// A thread holds 8 neighbouring elements of one row, d_head / 8 threads a row, K and V of a head side by side; the threads of
+// a position are whole warps, so a warp looks its position up once.  What bounds both directions is the row
+// traffic; a warp has its own loads in flight before it looks up where they go.
+#include "paged.cuh"
+#include <cuda_fp8.h>
+
+namespace csd {
+
+struct RowsView { const void* k; const void* v; long long ld; };
+
+// Sequence that row r of the batch belongs to, its lengths, and the row's position; false: to none.  Whole warps.
+__device__ __forceinline__ bool find_row(const PagedView& w, int r, int* seq, int* pos) {
+    const int lane = threadIdx.x & 31;
+    int s = 0;
+    for (int b = 0; b < w.n_seqs; b += 32) {
+        const bool past = b + lane < w.n_seqs && w.row_start[b + lane + 1] <= r;
+        const int n = __popc(__ballot_sync(0xffffffffu, past));
+        s += n;
+        if (n < 32) break;
+    }
+    if (s >= w.n_seqs) return false;
+    const PagedSeq q = paged_seq(w, s);
+    *seq = s; *pos = q.kv + r - q.start;
+    return r >= q.start && r - q.start < q.rows;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* p, float* x) {
+    if constexpr (BF16) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        x[0] = bf16lo(u.x); x[1] = bf16hi(u.x); x[2] = bf16lo(u.y); x[3] = bf16hi(u.y);
+        x[4] = bf16lo(u.z); x[5] = bf16hi(u.z); x[6] = bf16lo(u.w); x[7] = bf16hi(u.w);
+    } else {
+        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+}
+
+__device__ __forceinline__ uint4 pack8_bf16(const float* x) {
+    auto two = [](float a, float b) { return (uint32_t)float_to_bf16_bits(a) | (uint32_t)float_to_bf16_bits(b) << 16; };
+    return make_uint4(two(x[0], x[1]), two(x[2], x[3]), two(x[4], x[5]), two(x[6], x[7]));
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store8(void* p, const float* x) {
+    if constexpr (BF16) {
+        *reinterpret_cast<uint4*>(p) = pack8_bf16(x);
+    } else {
+        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+}
+
+// Which row, head and half (K or V) a thread has: warps_per_row whole warps a row of the batch.
+template <int DH> struct Part {
+    int r, head, which, col;
+    bool live;
+    __device__ __forceinline__ Part(int heads, int warps_per_row) {
+        const int gw = (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5));
+        r = gw / warps_per_row;
+        const int i = (gw % warps_per_row) * 32 + (threadIdx.x & 31), unit = i / (DH / 8);
+        head = unit >> 1; which = unit & 1; col = i % (DH / 8) * 8;
+        live = head < heads;
+    }
+};
+
+template <int DH, bool ROWS16, bool E4M3>
+__global__ void __launch_bounds__(256)
+paged_append_kernel(const PagedView w, const RowsView src, int warps_per_row) {
+    pdl_wait();
+    pdl_trigger();
+    const Part<DH> p(w.heads, warps_per_row);
+    if (p.r >= w.total_rows) return;
+    float x[8] = {};
+    if (p.live) {
+        const size_t at = (size_t)p.r * src.ld + p.head * DH + p.col;
+        load8<ROWS16>((const char*)(p.which ? src.v : src.k) + at * (ROWS16 ? 2 : 4), x);
+    }
+    int seq, pos;
+    if (!find_row(w, p.r, &seq, &pos)) return;
+    const int page = paged_page(w, seq, pos);
+    if (page < 0) return;
+    const size_t row = paged_row(w, page, p.head, pos);
+    unsigned char* pool = const_cast<unsigned char*>(p.which ? w.v : w.k);
+    if constexpr (!E4M3) {
+        if (p.live) *reinterpret_cast<uint4*>(pool + (row * DH + p.col) * 2) = pack8_bf16(x);
+    } else {
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float a = fabsf(x[i]);
+            top = fmaxf(top, a < INFINITY ? a : 0.f);                // (NaN fails the comparison)
+        }
+#pragma unroll
+        for (int o = DH / 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const unsigned bits = __float_as_uint(top);
+        const int e = max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 27);        // exponent of the scale + 127
+        if (e == 247) {                                              // (up to 240 * 2^120: the next number, 2^128, is none in fp32)
+            const float most = __uint_as_float(0x7f700000u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = x[i] > most ? most : x[i] < -most ? -most : x[i];
+        }
+        const float inv = __uint_as_float((unsigned)(254 - e) << 23);
+        uint32_t out[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const __nv_fp8x2_storage_t a = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i] * inv, x[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+            const __nv_fp8x2_storage_t b = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i + 2] * inv, x[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+            out[i] = (uint32_t)a | (uint32_t)b << 16;
+        }
+        if (p.live) {
+            *reinterpret_cast<uint2*>(pool + row * DH + p.col) = make_uint2(out[0], out[1]);
+            if (p.col == 0) const_cast<uint8_t*>(p.which ? w.v_exp : w.k_exp)[row] = (uint8_t)e;
+        }
+    }
+}
+
+template <int DH, bool ROWS16, bool E4M3>
+__global__ void __launch_bounds__(256)
+paged_read_kernel(const PagedView w, const RowsView dst, int warps_per_row) {
+    pdl_wait();
+    pdl_trigger();
+    const Part<DH> p(w.heads, warps_per_row);
+    if (p.r >= w.total_rows) return;
+    int seq, pos;
+    if (!find_row(w, p.r, &seq, &pos) || !p.live) return;
+    const int page = paged_page(w, seq, pos);
+    float x[8] = {};
+    if (page >= 0) {
+        const size_t row = paged_row(w, page, p.head, pos);
+        const unsigned char* pool = p.which ? w.v : w.k;
+        if constexpr (!E4M3) {
+            load8<true>(pool + (row * DH + p.col) * 2, x);
+        } else {
+            const float scale = exp_scale((p.which ? w.v_exp : w.k_exp)[row]);
+            const uint2 u = *reinterpret_cast<const uint2*>(pool + row * DH + p.col);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __half2 h(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((i < 2 ? u.x : u.y) >> 16 * (i & 1)), __NV_E4M3));
+                const float2 f = __half22float2(h);
+                x[2 * i] = f.x * scale; x[2 * i + 1] = f.y * scale;
+            }
+        }
+    }
+    const size_t at = (size_t)p.r * dst.ld + p.head * DH + p.col;
+    store8<ROWS16>((char*)const_cast<void*>(p.which ? dst.v : dst.k) + at * (ROWS16 ? 2 : 4), x);
+}
+
+template <template <int, bool, bool> class Pick>
+static csd_status launch_cache(const PagedView& w, const RowsView& rows, int d_head, bool rows16, cudaStream_t st) {
+    const int warps_per_row = (2 * w.heads * (d_head / 8) + 31) / 32;
+    const long long warps = (long long)w.total_rows * warps_per_row, blocks = (warps + 7) / 8;
+    if (blocks >= 1ll << 31) return CSD_ERR_INVALID_ARG;
+    PdlLaunch L(dim3((unsigned)blocks), dim3(256), 0, st);
+    auto go = [&](auto kern) { return cudaLaunchKernelEx(&L.cfg, kern, w, rows, warps_per_row); };
+    const bool e4m3 = w.k_exp != nullptr;
+    cudaError_t e;
+    if (d_head == 64)
+        e = rows16 ? (e4m3 ? go(Pick<64, true, true>::kernel) : go(Pick<64, true, false>::kernel))
+                   : (e4m3 ? go(Pick<64, false, true>::kernel) : go(Pick<64, false, false>::kernel));
+    else
+        e = rows16 ? (e4m3 ? go(Pick<128, true, true>::kernel) : go(Pick<128, true, false>::kernel))
+                   : (e4m3 ? go(Pick<128, false, true>::kernel) : go(Pick<128, false, false>::kernel));
+    CSD_CUDA(e);
+    count_launch();
+    return CSD_OK;
+}
+
+template <int DH, bool R, bool E> struct AppendPick { static constexpr auto kernel = paged_append_kernel<DH, R, E>; };
+template <int DH, bool R, bool E> struct ReadPick { static constexpr auto kernel = paged_read_kernel<DH, R, E>; };
+
+template <template <int, bool, bool> class Pick>
+static csd_status run_cache(const csd_kv_pool* pool, const csd_paged_batch* batch, const void* k, const void* v, int64_t ld,
+                            int row_type, void* stream) {
+    PagedView w;
+    const csd_status ok = paged_view(pool, batch, &w);
+    if (ok != CSD_OK) return ok;
+    const int64_t width = (int64_t)pool->n_kv_heads * pool->d_head;
+    if (row_type != CSD_F32 && row_type != CSD_BF16) return CSD_ERR_INVALID_ARG;
+    if (w.total_rows == 0) return CSD_OK;
+    if (!paged_rows_ok(k, ld, width) || !paged_rows_ok(v, ld, width)) return CSD_ERR_INVALID_ARG;
+    w.status = status_word_device();
+    if (!w.status) return CSD_ERR_CUDA;
+    return launch_cache<Pick>(w, RowsView{k, v, ld}, pool->d_head, row_type == CSD_BF16, (cudaStream_t)stream);
+}
+
+}  // namespace csd
+
+using namespace csd;
+
+extern "C" csd_status csd_paged_append(const csd_kv_pool* pool, const csd_paged_batch* batch, const void* k_dev, const void* v_dev,
+                                       int64_t ld, int row_type, void* stream) {
+    return run_cache<AppendPick>(pool, batch, k_dev, v_dev, ld, row_type, stream);
+}
+
+extern "C" csd_status csd_paged_read(const csd_kv_pool* pool, const csd_paged_batch* batch, void* k_dev, void* v_dev, int64_t ld,
+                                     int row_type, void* stream) {
+    return run_cache<ReadPick>(pool, batch, k_dev, v_dev, ld, row_type, stream);
+}

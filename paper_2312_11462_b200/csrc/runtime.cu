@@ -57,6 +57,7 @@ extern "C" const char* csd_status_string(csd_status s) {
         case CSD_ERR_BAD_TOKEN: return "token id outside the vocabulary";
         case CSD_ERR_TIMEOUT: return "bounded device loop reached its limit";
         case CSD_ERR_UNSUPPORTED: return "unsupported";
+        case CSD_ERR_BAD_PAGE: return "page id outside the pool";
     }
     return "unknown status";
 }
