@@ -288,8 +288,8 @@ csd_status csd_spec_verify(const void* target_probs_dev, int64_t ld_p, const voi
  *                values are the numbers times 2^e, e the smallest whole number, at least -100, with
  *                max|x| <= 448 * 2^e over the row's finite entries (a power of two: scaling rounds
  *                nothing, and a stored value is exact in fp32 and bf16).  Infinities become
- *                +-448 * 2^e, NaN stays NaN; at e = 120 the
- *                numbers end at 240 (256 * 2^120 is none in fp32).
+ *                +-448 * 2^e; at e = 120 the numbers end at 240
+ *                (256 * 2^120 is none in fp32).  A row with a NaN gets the byte 255 and is NaN.
  * A batch is a chunk of new rows for each sequence: rows row_start[s] .. row_start[s+1] - 1 of the
  * packed row arrays are sequence s at positions kv_len[s] .., kv_len[s] positions lie before them.
  * The arrays are on the device, so a captured call replays with other lengths.  Lengths of zero are
@@ -309,7 +309,7 @@ typedef struct {
     int32_t d_head;       /* 64 or 128                                                */
     void* k_dev;          /* [n_pages][n_kv_heads][page_size][d_head], 16-byte aligned */
     void* v_dev;
-    uint8_t* k_exp_dev;   /* CSD_KV_E4M3: [n_pages][n_kv_heads][page_size], else NULL */
+    uint8_t* k_exp_dev;   /* CSD_KV_E4M3: [n_pages][n_kv_heads][page_size], 16-byte aligned */
     uint8_t* v_exp_dev;
 } csd_kv_pool;
 

@@ -24,7 +24,9 @@ inline csd_status paged_view(const csd_kv_pool* pool, const csd_paged_batch* bat
     if ((1 << shift) != pool->page_size) return CSD_ERR_SHAPE;
     if ((long long)pool->n_pages * pool->n_kv_heads >= (1ll << 31) >> shift) return CSD_ERR_SHAPE;
     if (!pool->k_dev || !pool->v_dev || (((uintptr_t)pool->k_dev) & 15) || (((uintptr_t)pool->v_dev) & 15)) return CSD_ERR_INVALID_ARG;
-    if (pool->kind == CSD_KV_E4M3 && (!pool->k_exp_dev || !pool->v_exp_dev)) return CSD_ERR_INVALID_ARG;
+    if (pool->kind == CSD_KV_E4M3 &&
+        (!pool->k_exp_dev || !pool->v_exp_dev || (((uintptr_t)pool->k_exp_dev) & 15) || (((uintptr_t)pool->v_exp_dev) & 15)))
+        return CSD_ERR_INVALID_ARG;
     if (batch->n_seqs < 1 || batch->n_seqs > CSD_MAX_SEQS || batch->max_pages < 1 || batch->total_rows < 0 || batch->max_rows < 1)
         return CSD_ERR_INVALID_ARG;
     if ((long long)batch->max_pages << shift >= 1ll << 30) return CSD_ERR_INVALID_ARG;
@@ -72,7 +74,7 @@ __device__ __forceinline__ size_t paged_row(const PagedView& w, int page, int he
     return ((size_t)page * w.heads + head << w.page_shift) + (t & ((1 << w.page_shift) - 1));
 }
 
-// 2^(byte - 127) for the bytes that append writes (27 .. 247); others come from positions nobody has written
-__device__ __forceinline__ float exp_scale(unsigned e) { return __uint_as_float(e << 23); }
+// Scale of an 8-bit row: 2^(e - 127), NaN for 255.
+__device__ __forceinline__ float row_scale(unsigned e) { return __uint_as_float(e << 23 | (e == 255u ? 1u << 22 : 0u)); }
 
 }  // namespace csd

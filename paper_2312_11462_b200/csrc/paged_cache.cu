@@ -1,7 +1,7 @@
 // Writing rows into the paged cache, in 16 or 8 bits, and reading them back.
 //
 // A row of one position and head is quantised by the lanes that hold it: max|x| by a shuffle among them, the scale's exponent
-// from the maximum's bits (max|x| = m * 2^x with m in [1, 2): 448 = 1.75 * 2^8, so e = x - 8, one more where m > 1.75), then
+// from the maximum's bits (of finite entries; max|x| = m * 2^x with m in [1, 2): 448 = 1.75 * 2^8, so e = x - 8, one more where m > 1.75), then
 // rn_e4m3(x * 2^-e).  The scale is a power of two, so x * 2^-e is exact and the result does not depend on how it is formed.
 //
 // A thread holds 8 neighbouring elements of one row, d_head / 8 threads a row, K and V of a head side by side; the threads of
@@ -91,16 +91,16 @@ paged_append_kernel(const PagedView w, const RowsView src, int warps_per_row) {
     if constexpr (!E4M3) {
         if (p.live) *reinterpret_cast<uint4*>(pool + (row * DH + p.col) * 2) = pack8_bf16(x);
     } else {
-        float top = 0.f;
+        unsigned bits = 0u;                                          // of the largest finite |x|, or a NaN's, which is larger
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float a = fabsf(x[i]);
-            top = fmaxf(top, a < INFINITY ? a : 0.f);                // (NaN fails the comparison)
+            const unsigned b = __float_as_uint(x[i]) & 0x7fffffffu;
+            bits = max(bits, b == 0x7f800000u ? 0u : b);
         }
 #pragma unroll
-        for (int o = DH / 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const unsigned bits = __float_as_uint(top);
-        const int e = max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 27);        // exponent of the scale + 127
+        for (int o = DH / 16; o > 0; o >>= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, o));
+        const bool nan = bits > 0x7f800000u;
+        const int e = nan ? 127 : max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 27);        // exponent of the scale + 127
         if (e == 247) {                                              // (up to 240 * 2^120: the next number, 2^128, is none in fp32)
             const float most = __uint_as_float(0x7f700000u);
 #pragma unroll
@@ -116,7 +116,7 @@ paged_append_kernel(const PagedView w, const RowsView src, int warps_per_row) {
         }
         if (p.live) {
             *reinterpret_cast<uint2*>(pool + row * DH + p.col) = make_uint2(out[0], out[1]);
-            if (p.col == 0) const_cast<uint8_t*>(p.which ? w.v_exp : w.k_exp)[row] = (uint8_t)e;
+            if (p.col == 0) const_cast<uint8_t*>(p.which ? w.v_exp : w.k_exp)[row] = (uint8_t)(nan ? 255 : e);
         }
     }
 }
@@ -138,7 +138,7 @@ paged_read_kernel(const PagedView w, const RowsView dst, int warps_per_row) {
         if constexpr (!E4M3) {
             load8<true>(pool + (row * DH + p.col) * 2, x);
         } else {
-            const float scale = exp_scale((p.which ? w.v_exp : w.k_exp)[row]);
+            const float scale = row_scale((p.which ? w.v_exp : w.k_exp)[row]);
             const uint2 u = *reinterpret_cast<const uint2*>(pool + row * DH + p.col);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {

@@ -19,7 +19,7 @@ def quantise(x):
     most = np.where(e == 120, 240.0, 448.0)[..., None]           # 256 * 2^120 is no fp32 number
     y = np.clip(np.where(np.isnan(x), 0.0, x) / unit, -most, most)
     step = np.exp2(np.maximum(np.floor(np.log2(np.maximum(np.abs(y), 2.0 ** -30))), -6.0) - 3.0)
-    return np.where(np.isnan(x), np.nan, np.round(y / step) * step * unit), e
+    return np.where(np.isnan(x).any(-1, keepdims=True), np.nan, np.round(y / step) * step * unit), e
 
 
 class Case:

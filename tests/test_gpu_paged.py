@@ -73,6 +73,7 @@ def test_rows_of_every_size(b):
         assert np.array_equal(np.isnan(g), np.isnan(want)) and np.array_equal(g[~np.isnan(g)], want[~np.isnan(want)])
     _, e = pp.quantise(x.double().numpy())
     at = torch.arange(64)
+    e = np.where(np.isnan(x.numpy()).any(-1), 128, e)
     assert np.array_equal(c.pool.k_exp.cpu()[c.table[0, at // 16].long(), :, at % 16].numpy().astype(int) - 127, e)
 
 

@@ -16,7 +16,7 @@ def test_quantised_rows():
     assert np.array_equal(again, y) and (e2 <= e).all()
     y, e = pp.quantise(np.array([[0.0] * 8, [448.0] * 8, [448.1] * 8, [np.inf] + [1.0] * 7, [np.nan] + [3.0] * 7]))
     assert list(e[:3]) == [-100, 0, 1] and (y[0] == 0).all() and (y[1] == 448).all()
-    assert y[3, 0] == 448.0 * 2.0 ** e[3] and np.isnan(y[4, 0]) and (y[4, 1:] == 3).all()
+    assert y[3, 0] == 448.0 * 2.0 ** e[3] and np.isnan(y[4]).all()
     # the e4m3 numbers themselves, against torch's conversion
     z = torch.linspace(-448, 448, 20001, dtype=torch.float64)
     z[0] = -448

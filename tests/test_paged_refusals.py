@@ -29,6 +29,7 @@ def batch(b, **kw):
 BAD_POOLS = [(dict(kind=2), INVALID), (dict(n_pages=0), INVALID), (dict(page_size=24), SHAPE), (dict(page_size=8), SHAPE), (dict(page_size=256), SHAPE),
              (dict(page_size=0), SHAPE), (dict(n_kv_heads=0), INVALID), (dict(d_head=96), SHAPE), (dict(d_head=32), SHAPE), (dict(k_dev=None), INVALID),
              (dict(v_dev=None), INVALID), (dict(k_dev=(1 << 20) + 8), INVALID), (dict(kind=1), INVALID), (dict(kind=1, k_exp_dev=4096), INVALID),
+             (dict(kind=1, k_exp_dev=4096, v_exp_dev=4104), INVALID),
              (dict(n_pages=1 << 26), SHAPE)]
 BAD_BATCHES = [(dict(n_seqs=0), INVALID), (dict(n_seqs=1025), INVALID), (dict(max_pages=0), INVALID), (dict(max_pages=1 << 27), INVALID),
                (dict(total_rows=-1), INVALID), (dict(max_rows=0), INVALID), (dict(page_table_dev=None), INVALID), (dict(row_start_dev=None), INVALID),
