@@ -4,10 +4,10 @@
 // from the maximum's bits (of finite entries; max|x| = m * 2^x with m in [1, 2): 448 = 1.75 * 2^8, so e = x - 8, one more where m > 1.75), then
 // rn_e4m3(x * 2^-e).  The scale is a power of two, so x * 2^-e is exact and the result does not depend on how it is formed.
 //
-// A thread holds 8 neighbouring elements of one row, d_head / 8 threads a row, K and V of a head side by side; the threads of
-// a position are whole warps, so a warp looks its position up once.  What bounds both directions is the row
-// traffic; a warp has its own loads in flight before it looks up where they go.
+// A thread holds 8 neighbouring elements of one row, d_head / 8 threads a row, K and V of a head side by side; a warp belongs to
+// one position and looks it up once.  What bounds both directions is the row traffic.
 #include "paged.cuh"
+#include "tc_common.cuh"
 #include <cuda_fp8.h>
 
 namespace csd {
@@ -57,108 +57,146 @@ __device__ __forceinline__ void store8(void* p, const float* x) {
     }
 }
 
-// Which row, head and half (K or V) a thread has: warps_per_row whole warps a row of the batch.
-template <int DH> struct Part {
-    int r, head, which, col;
-    bool live;
-    __device__ __forceinline__ Part(int heads, int warps_per_row) {
-        const int gw = (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5));
-        r = gw / warps_per_row;
-        const int i = (gw % warps_per_row) * 32 + (threadIdx.x & 31), unit = i / (DH / 8);
-        head = unit >> 1; which = unit & 1; col = i % (DH / 8) * 8;
-        live = head < heads;
-    }
+// A position's units of eight elements: [head][K, V][column].  `split` warps share a position, each takes every split-th stretch of 32
+// units, BATCH stretches at a time with their loads in flight together.
+constexpr int BATCH = 4;
+template <int DH> struct Unit {
+    int head, which, col;
+    __device__ __forceinline__ explicit Unit(int i) : head(i / (2 * (DH / 8))), which(i / (DH / 8) & 1), col(i % (DH / 8) * 8) {}
 };
 
 template <int DH, bool ROWS16, bool E4M3>
 __global__ void __launch_bounds__(256)
-paged_append_kernel(const PagedView w, const RowsView src, int warps_per_row) {
+paged_append_kernel(const PagedView w, const RowsView src, int split) {
     pdl_wait();
     pdl_trigger();
-    const Part<DH> p(w.heads, warps_per_row);
-    if (p.r >= w.total_rows) return;
-    float x[8] = {};
-    if (p.live) {
-        const size_t at = (size_t)p.r * src.ld + p.head * DH + p.col;
-        load8<ROWS16>((const char*)(p.which ? src.v : src.k) + at * (ROWS16 ? 2 : 4), x);
-    }
-    int seq, pos;
-    if (!find_row(w, p.r, &seq, &pos)) return;
-    const int page = paged_page(w, seq, pos);
-    if (page < 0) return;
-    const size_t row = paged_row(w, page, p.head, pos);
-    unsigned char* pool = const_cast<unsigned char*>(p.which ? w.v : w.k);
-    if constexpr (!E4M3) {
-        if (p.live) *reinterpret_cast<uint4*>(pool + (row * DH + p.col) * 2) = pack8_bf16(x);
-    } else {
-        unsigned bits = 0u;                                          // of the largest finite |x|, or a NaN's, which is larger
+    const int gw = (int)(blockIdx.x * 8 + (threadIdx.x >> 5)), r = gw / split, lane = threadIdx.x & 31;
+    const int units = 2 * w.heads * (DH / 8), step = 32 * split;
+    if (r >= w.total_rows) return;
+    int page = -1, pos = 0;
+    bool looked = false;
+    for (int u0 = gw % split * 32; u0 < units; u0 += BATCH * step) {
+        float x[BATCH][8] = {};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const unsigned b = __float_as_uint(x[i]) & 0x7fffffffu;
-            bits = max(bits, b == 0x7f800000u ? 0u : b);
+        for (int b = 0; b < BATCH; ++b) {
+            const Unit<DH> p(u0 + b * step + lane);
+            if (p.head < w.heads) {
+                const size_t at = (size_t)r * src.ld + p.head * DH + p.col;
+                load8<ROWS16>((const char*)(p.which ? src.v : src.k) + at * (ROWS16 ? 2 : 4), x[b]);
+            }
+        }
+        if (!looked) {                                               // (the first loads are under way)
+            int seq;
+            if (!find_row(w, r, &seq, &pos)) return;
+            page = paged_page(w, seq, pos);
+            if (page < 0) return;
+            looked = true;
         }
 #pragma unroll
-        for (int o = DH / 16; o > 0; o >>= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, o));
-        const bool nan = bits > 0x7f800000u;
-        const int e = nan ? 127 : max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 27);        // exponent of the scale + 127
-        if (e == 247) {                                              // (up to 240 * 2^120: the next number, 2^128, is none in fp32)
-            const float most = __uint_as_float(0x7f700000u);
+        for (int b = 0; b < BATCH; ++b) {
+            const Unit<DH> p(u0 + b * step + lane);
+            const bool live = p.head < w.heads;
+            const size_t row = paged_row(w, page, live ? p.head : 0, pos);
+            unsigned char* pool = const_cast<unsigned char*>(p.which ? w.v : w.k);
+            if constexpr (!E4M3) {
+                if (live) *reinterpret_cast<uint4*>(pool + (row * DH + p.col) * 2) = pack8_bf16(x[b]);
+            } else {
+                unsigned bits = 0u;                                  // of the largest finite |x|, or a NaN's, which is larger
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] > most ? most : x[i] < -most ? -most : x[i];
-        }
-        const float inv = __uint_as_float((unsigned)(254 - e) << 23);
-        uint32_t out[2];
+                for (int i = 0; i < 8; ++i) {
+                    const unsigned v = __float_as_uint(x[b][i]) & 0x7fffffffu;
+                    bits = max(bits, v == 0x7f800000u ? 0u : v);
+                }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const __nv_fp8x2_storage_t a = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i] * inv, x[4 * i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-            const __nv_fp8x2_storage_t b = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i + 2] * inv, x[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-            out[i] = (uint32_t)a | (uint32_t)b << 16;
-        }
-        if (p.live) {
-            *reinterpret_cast<uint2*>(pool + row * DH + p.col) = make_uint2(out[0], out[1]);
-            if (p.col == 0) const_cast<uint8_t*>(p.which ? w.v_exp : w.k_exp)[row] = (uint8_t)(nan ? 255 : e);
+                for (int o = DH / 16; o > 0; o >>= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, o));
+                const bool nan = bits > 0x7f800000u;
+                const int e = nan ? 127 : max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 27);        // exponent of the scale + 127
+                if (e == 247) {                                      // (up to 240 * 2^120: the next number, 2^128, is none in fp32)
+                    const float most = __uint_as_float(0x7f700000u);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[b][i] = x[b][i] > most ? most : x[b][i] < -most ? -most : x[b][i];
+                }
+                const float inv = __uint_as_float((unsigned)(254 - e) << 23);
+                uint32_t out[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float* y = x[b] + 4 * i;
+                    const __nv_fp8x2_storage_t f = __nv_cvt_float2_to_fp8x2(make_float2(y[0] * inv, y[1] * inv), __NV_SATFINITE, __NV_E4M3);
+                    const __nv_fp8x2_storage_t g = __nv_cvt_float2_to_fp8x2(make_float2(y[2] * inv, y[3] * inv), __NV_SATFINITE, __NV_E4M3);
+                    out[i] = (uint32_t)f | (uint32_t)g << 16;
+                }
+                if (live) {
+                    *reinterpret_cast<uint2*>(pool + row * DH + p.col) = make_uint2(out[0], out[1]);
+                    if (p.col == 0) const_cast<uint8_t*>(p.which ? w.v_exp : w.k_exp)[row] = (uint8_t)(nan ? 255 : e);
+                }
+            }
         }
     }
 }
 
 template <int DH, bool ROWS16, bool E4M3>
 __global__ void __launch_bounds__(256)
-paged_read_kernel(const PagedView w, const RowsView dst, int warps_per_row) {
+paged_read_kernel(const PagedView w, const RowsView dst, int split) {
     pdl_wait();
     pdl_trigger();
-    const Part<DH> p(w.heads, warps_per_row);
-    if (p.r >= w.total_rows) return;
+    const int gw = (int)(blockIdx.x * 8 + (threadIdx.x >> 5)), r = gw / split, lane = threadIdx.x & 31;
+    const int units = 2 * w.heads * (DH / 8), step = 32 * split;
+    if (r >= w.total_rows) return;
     int seq, pos;
-    if (!find_row(w, p.r, &seq, &pos) || !p.live) return;
+    if (!find_row(w, r, &seq, &pos)) return;
     const int page = paged_page(w, seq, pos);
-    float x[8] = {};
-    if (page >= 0) {
-        const size_t row = paged_row(w, page, p.head, pos);
-        const unsigned char* pool = p.which ? w.v : w.k;
-        if constexpr (!E4M3) {
-            load8<true>(pool + (row * DH + p.col) * 2, x);
-        } else {
-            const float scale = row_scale((p.which ? w.v_exp : w.k_exp)[row]);
-            const uint2 u = *reinterpret_cast<const uint2*>(pool + row * DH + p.col);
+    for (int u0 = gw % split * 32; u0 < units; u0 += BATCH * step) {
+        uint4 raw[BATCH];
+        unsigned e[BATCH];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __half2 h(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((i < 2 ? u.x : u.y) >> 16 * (i & 1)), __NV_E4M3));
-                const float2 f = __half22float2(h);
-                x[2 * i] = f.x * scale; x[2 * i + 1] = f.y * scale;
+        for (int b = 0; b < BATCH; ++b) {
+            const Unit<DH> p(u0 + b * step + lane);
+            raw[b] = make_uint4(0u, 0u, 0u, 0u);
+            e[b] = 127u;
+            if (p.head >= w.heads || page < 0) continue;
+            const size_t row = paged_row(w, page, p.head, pos);
+            const unsigned char* pool = p.which ? w.v : w.k;
+            if constexpr (E4M3) {
+                const uint2 u = *reinterpret_cast<const uint2*>(pool + row * DH + p.col);
+                raw[b].x = u.x; raw[b].y = u.y;
+                e[b] = (p.which ? w.v_exp : w.k_exp)[row];
+            } else {
+                raw[b] = *reinterpret_cast<const uint4*>(pool + (row * DH + p.col) * 2);
             }
         }
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            const Unit<DH> p(u0 + b * step + lane);
+            if (p.head >= w.heads) continue;
+            float x[8];
+            if constexpr (E4M3) {
+                const float scale = row_scale(e[b]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const __half2 h(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((i < 2 ? raw[b].x : raw[b].y) >> 16 * (i & 1)), __NV_E4M3));
+                    const float2 f = __half22float2(h);
+                    x[2 * i] = f.x * scale; x[2 * i + 1] = f.y * scale;
+                }
+            } else {
+                load8<true>(&raw[b], x);
+            }
+            const size_t at = (size_t)r * dst.ld + p.head * DH + p.col;
+            store8<ROWS16>((char*)const_cast<void*>(p.which ? dst.v : dst.k) + at * (ROWS16 ? 2 : 4), x);
+        }
     }
-    const size_t at = (size_t)p.r * dst.ld + p.head * DH + p.col;
-    store8<ROWS16>((char*)const_cast<void*>(p.which ? dst.v : dst.k) + at * (ROWS16 ? 2 : 4), x);
 }
 
 template <template <int, bool, bool> class Pick>
 static csd_status launch_cache(const PagedView& w, const RowsView& rows, int d_head, bool rows16, cudaStream_t st) {
-    const int warps_per_row = (2 * w.heads * (d_head / 8) + 31) / 32;
-    const long long warps = (long long)w.total_rows * warps_per_row, blocks = (warps + 7) / 8;
-    if (blocks >= 1ll << 31) return CSD_ERR_INVALID_ARG;
+    // warps a position: all its stretches at once while that leaves SMs idle, down to one, which looks up where the position lies
+    // once for all of them (9000 positions of 32 heads x 128, bf16 to 8 bits and back: 184 us with a warp a stretch)
+    const int stretches = (2 * w.heads * (d_head / 8) + 31) / 32;
+    int split = stretches;
+    while (split > 1 && (long long)w.total_rows * ((split + 1) / 2) >= 48ll * tc_sm_count()) split = (split + 1) / 2;
+    const long long warps = (long long)w.total_rows * split, blocks = (warps + 7) / 8;
+    if (warps >= 1ll << 31) return CSD_ERR_INVALID_ARG;
     PdlLaunch L(dim3((unsigned)blocks), dim3(256), 0, st);
-    auto go = [&](auto kern) { return cudaLaunchKernelEx(&L.cfg, kern, w, rows, warps_per_row); };
+    auto go = [&](auto kern) { return cudaLaunchKernelEx(&L.cfg, kern, w, rows, split); };
     const bool e4m3 = w.k_exp != nullptr;
     cudaError_t e;
     if (d_head == 64)

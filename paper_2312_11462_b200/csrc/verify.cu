@@ -1,5 +1,13 @@
-// Verification of drafted tokens against given probabilities with given random numbers: a CTA a row.
-#include "common.cuh"
+// Verification of drafted tokens against given probabilities with given random numbers.
+//
+// A row needs 2 k numbers for its tests and then one law, or two, of V entries: what is left of p after a rejection, max(0, p - q),
+// summed in fp64 (the differences of fp32 numbers are exact there, and so are most sums), and the entry in which u of the
+// whole falls.  A cluster of up to eight CTAs takes a row.  Every CTA makes the row's tests (a warp, a lane a draft), each warp sums a
+// contiguous piece of the law, the warps' sums go to all CTAs through distributed shared memory, and the warp whose piece holds
+// the target goes through it once more (from L2): lanes' stretches, then the stretch.  No workspace, one launch.
+//
+// What bounds it: many rows, the laws' bytes; one row, the chain of tests, sums, exchange and second look.
+#include "tc_common.cuh"
 
 namespace csd {
 
@@ -10,78 +18,231 @@ struct VerifyArgs {
     int k, V;
 };
 
-template <bool LAW16>
-__device__ __forceinline__ float law_at(const void* law, size_t i) {
+constexpr int VW = 16, VMAX = 8;           // warps of a CTA, CTAs of a cluster at most
+constexpr int VSUMS = VW * VMAX;
+
+template <bool LAW16> __device__ __forceinline__ float law_at(const void* law, size_t i) {
     return LAW16 ? bf16_bits_to_float(((const uint16_t*)law)[i]) : ((const float*)law)[i];
 }
-
 // what an entry carries: positive finite numbers only
-__device__ __forceinline__ double mass_of(double x) { return x > 0.0 && x < INFINITY ? x : 0.0; }
-// entry j of what is left of p after a rejection
-__device__ __forceinline__ double left_of(float p, float q) { return fmax(mass_of(p) - mass_of(q), 0.0); }
+__device__ __forceinline__ float mass_of(float x) { return x > 0.f && x < INFINITY ? x : 0.f; }
 
-constexpr int VT = 1024;
+// A sum of differences max(0, x - y), x and y >= 0, in a pair of fp32 numbers: x - y and each sum keep their rounding errors (the
+// differences by x >= y, the sums without a condition), so that about 46 bits of a lane's hundred entries are right.  In
+// fp64 the conversions and sums bound the pass: 256 rows of 128256 entries 120 us.
+struct Pair {
+    float hi = 0.f, lo = 0.f;
+    __device__ __forceinline__ void add(float x, float y) {
+        const float d = x > y ? x - y : 0.f, e = x > y ? (x - d) - y : 0.f;
+        const float t = hi + d, z = t - hi;
+        lo += ((hi - (t - z)) + (d - z)) + e;
+        hi = t;
+    }
+    __device__ __forceinline__ double value() const { return (double)hi + (double)lo; }
+};
+
+__device__ __forceinline__ double warp_scan(double x, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
 
 template <bool LAW16>
-__global__ void __launch_bounds__(VT)
+__global__ void __launch_bounds__(32 * VW, 2)
 verify_kernel(const VerifyArgs a) {
-    __shared__ double part[VT];
-    __shared__ double s_total;
-    __shared__ int s_token;
-    const int row = blockIdx.x, tid = threadIdx.x, V = a.V;
-    int n = a.n_drafts ? a.n_drafts[row] : a.k;
-    if (n < 0 || n > a.k) { if (tid == 0) set_status(a.status, CSD_ERR_INVALID_ARG); n = min(max(n, 0), a.k); }
-    auto uniform = [&](int i) {
-        const float u = a.u[(size_t)row * (a.k + 1) + i];
-        if (!(u >= 0.f && u < 1.f)) { if (tid == 0) set_status(a.status, CSD_ERR_INVALID_ARG); return u >= 1.f ? 0.99999994f : 0.f; }
-        return u;
+    __shared__ double sums[2][VSUMS];      // of both forms of the law: the warps of the cluster in their order
+    __shared__ double stretch[VW];
+    __shared__ int s_at, s_n;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, V = a.V, k = a.k;
+    int ctas, rank;
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    const int row = blockIdx.x / ctas;
+    asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");      // (waited for before the first store to another CTA: all have begun)
+    pdl_wait();
+    pdl_trigger();
+    const int32_t* tokens = a.tokens + (size_t)row * k;
+    const float* uniforms = a.u + (size_t)row * (k + 1);
+    auto uniform = [&](int i, bool tell) {
+        const float u = uniforms[i];
+        if (u >= 0.f && u < 1.f) return u;
+        if (tell) set_status(a.status, CSD_ERR_INVALID_ARG);
+        return u >= 1.f ? 0.99999994f : 0.f;
     };
-    int at = 0;
-    for (; at < n; ++at) {
-        const int x = a.tokens[(size_t)row * a.k + at];
-        if (x < 0 || x >= V) { if (tid == 0) set_status(a.status, CSD_ERR_BAD_TOKEN); break; }
-        const float px = law_at<LAW16>(a.p, ((size_t)row * (a.k + 1) + at) * a.ldp + x);
-        const float qx = a.q ? law_at<LAW16>(a.q, ((size_t)row * a.k + at) * a.ldq + x) : 1.f;
-        if (!((double)uniform(at) * (double)qx < (double)px)) break;
-    }
-    const size_t prow = ((size_t)row * (a.k + 1) + at) * a.ldp, qrow = ((size_t)row * a.k + at) * a.ldq;
-    const int drop = at < n ? a.tokens[(size_t)row * a.k + at] : -1;
-    const double u = uniform(a.k);
-    const int per = (V + VT - 1) / VT, lo = min(tid * per, V), hi = min(lo + per, V);
-    int token = 0;
-    for (int mode = at < n ? 0 : 1; mode < 2; ++mode) {        // 0: what is left after a rejection, 1: the target's law
-        auto entry = [&](int j) {
-            const float p = law_at<LAW16>(a.p, prow + j);
-            if (mode == 1) return mass_of(p);
-            return a.q ? left_of(p, law_at<LAW16>(a.q, qrow + j)) : (j == drop ? 0.0 : mass_of(p));
-        };
-        double s = 0.0;
-        for (int j = lo; j < hi; ++j) s += entry(j);
-        part[tid] = s;
-        if (tid == 0) s_token = 0;
-        __syncthreads();
-        if (tid == 0) {
-            double run = 0.0;
-            for (int i = 0; i < VT; ++i) { const double x = part[i]; part[i] = run; run += x; }
-            s_total = run;
-        }
-        __syncthreads();
-        if (s_total > 0.0) {
-            const double target = u * s_total;
-            double run = part[tid];
-            if (run <= target && run + s > target)
-                for (int j = lo; j < hi; ++j) {
-                    run += entry(j);
-                    if (run > target) { s_token = j; break; }
+    if (warp == 0) {
+        int n = a.n_drafts ? a.n_drafts[row] : k;
+        if (n < 0 || n > k) { set_status(a.status, CSD_ERR_INVALID_ARG); n = min(max(n, 0), k); }
+        int at = n;
+        for (int i0 = 0; i0 < n && at == n; i0 += 32) {
+            const int i = i0 + lane;
+            bool stop = false;
+            if (i < n) {
+                const int x = tokens[i];
+                if (x < 0 || x >= V) {
+                    stop = true;
+                } else {
+                    const float px = law_at<LAW16>(a.p, ((size_t)row * (k + 1) + i) * a.ldp + x);
+                    const float qx = a.q ? law_at<LAW16>(a.q, ((size_t)row * k + i) * a.ldq + x) : 1.f;
+                    stop = !((double)uniform(i, true) * (double)qx < (double)px);
                 }
-            __syncthreads();
-            token = s_token;
+            }
+            const unsigned any = __ballot_sync(0xffffffffu, stop);
+            if (any) at = i0 + __ffs(any) - 1;
+        }
+        if (lane == 0) {
+            s_at = at; s_n = n;
+            if (at < n && (tokens[at] < 0 || tokens[at] >= V)) set_status(a.status, CSD_ERR_BAD_TOKEN);
+        }
+    }
+    __syncthreads();
+    const int at = s_at, n = s_n;
+    const size_t prow = ((size_t)row * (k + 1) + at) * a.ldp, qrow = ((size_t)row * k + at) * a.ldq;
+    const int drop = at < n ? tokens[at] : -1;
+    const double u = (double)uniform(k, tid == 0);
+    // this warp's piece of the vocabulary: warps of the cluster in order
+    const long long all = (long long)ctas * VW, mine = (long long)rank * VW + warp;
+    const int lo = (int)(mine * V / all), hi = (int)((mine + 1) * V / all);
+    int32_t* out = a.out + (size_t)row * (k + 1);
+    if (rank == 0) {
+        if (tid <= k && tid != at) out[tid] = tid < at ? tokens[tid] : -1;
+        if (tid == 0) a.accepted[row] = at;
+    }
+    asm volatile("barrier.cluster.wait;" ::: "memory");
+    for (int mode = at < n ? (a.q ? 0 : 1) : 2;; mode = 2) {     // p less q, p without the draft, p
+        auto entry = [&](int j) -> double {
+            const float p = mass_of(law_at<LAW16>(a.p, prow + j));
+            if (mode == 2) return (double)p;
+            if (mode == 1) return j == drop ? 0.0 : (double)p;
+            const float q = mass_of(law_at<LAW16>(a.q, qrow + j));
+            return p > q ? (double)p - (double)q : 0.0;
+        };
+        Pair s0, s1;
+        int j = lo + lane;
+#pragma unroll 1
+        for (; j + 7 * 32 < hi; j += 8 * 32) {
+            float p[8], q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = law_at<LAW16>(a.p, prow + j + 32 * i);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = mode == 0 ? law_at<LAW16>(a.q, qrow + j + 32 * i) : 0.f;
+            if (mode == 1) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] = j + 32 * i == drop ? 0.f : p[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                s0.add(mass_of(p[i]), mass_of(q[i]));
+                s1.add(mass_of(p[i + 1]), mass_of(q[i + 1]));
+            }
+        }
+        double rest = 0.0;
+        for (; j < hi; j += 32) rest += entry(j);
+        const double sum = warp_sum(s0.value() + s1.value() + rest);
+        const int form = mode == 2 ? 1 : 0;
+        if (lane < ctas) {
+            const uint32_t there = map_to_cta(smem_u32(&sums[form][mine]), (uint32_t)lane);
+            asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(there), "d"(sum) : "memory");
+        }
+        cluster_barrier();
+        // every warp: the pieces' edges, four a lane, the whole, and the piece that holds the target
+        double edge[VSUMS / 32], run = 0.0;
+#pragma unroll
+        for (int i = 0; i < VSUMS / 32; ++i) {
+            const int w = lane * (VSUMS / 32) + i;
+            run += w < all ? sums[form][w] : 0.0;
+            edge[i] = run;
+        }
+        const double upto = warp_scan(run, lane), before = __shfl_up_sync(0xffffffffu, upto, 1);
+        const double base = lane ? before : 0.0;
+        double total = 0.0;
+#pragma unroll
+        for (int i = 0; i < VSUMS / 32; ++i) {
+            edge[i] += base;
+            total = edge[i];
+        }
+        total = __shfl_sync(0xffffffffu, total, 31);
+        if (!(total > 0.0)) {
+            if (mode != 2) continue;                 // nothing is left: the target's own law
+            if (rank == 0 && tid == 0) out[at] = 0;
             break;
         }
+        const double target = u * total;
+        // pieces that end at or before the target
+        int past = 0;
+#pragma unroll
+        for (int i = 0; i < VSUMS / 32; ++i) past += edge[i] <= target ? 1 : 0;
+        past = __reduce_add_sync(0xffffffffu, past);
+        if (past / VW != rank) break;                // (the same for all warps of a CTA)
+        // edge[] of the piece before that one
+        double left = 0.0;
+#pragma unroll
+        for (int i = 0; i < VSUMS / 32; ++i) {
+            const double e = __shfl_sync(0xffffffffu, edge[i], past > 0 ? (past - 1) / (VSUMS / 32) : 0);
+            if (past > 0 && (past - 1) % (VSUMS / 32) == i) left = e;
+        }
+        // The CTA's warps take a stretch of that piece each.  Where another order of the sums leaves the target behind the last
+        // entry, it is the last entry that carries anything.
+        const int f0 = (int)((long long)past * V / all), len = (int)((long long)(past + 1) * V / all) - f0;
+        const int g0 = f0 + (int)((long long)warp * len / VW), g1 = f0 + (int)((long long)(warp + 1) * len / VW);
+        const int per = (g1 - g0 + 31) / 32, b0 = min(g0 + lane * per, g1), b1 = min(b0 + per, g1);
+        double s = 0.0;
+#pragma unroll 8
+        for (int i = b0; i < b1; ++i) s += entry(i);
+        const double upto_lane = warp_scan(s, lane);
+        if (lane == 31) stretch[warp] = upto_lane;
         __syncthreads();
+        double want = target - left;
+        int pick = -1, some = 0;
+        for (int i = 0; i < VW; ++i) {
+            const double x = stretch[i];
+            if (x > 0.0) some = i;
+            if (pick < 0) {
+                if (x > want) pick = i; else want -= x;
+            }
+        }
+        if (pick < 0) { pick = some; want = INFINITY; }
+        if (pick != warp) break;
+        const unsigned here = __ballot_sync(0xffffffffu, upto_lane > want && s > 0.0), any = __ballot_sync(0xffffffffu, s > 0.0);
+        const int winner = here ? __ffs(here) - 1 : 31 - __clz(any);
+        if (lane == winner) {
+            double run_x = upto_lane - s;
+            int token = b0;
+            for (int i = b0; i < b1; ++i) {
+                const double x = entry(i);
+                if (!(x > 0.0)) continue;
+                token = i;
+                run_x += x;
+                if (run_x > want) break;
+            }
+            out[at] = token;
+        }
+        break;
     }
-    if (tid <= a.k) a.out[(size_t)row * (a.k + 1) + tid] = tid < at ? a.tokens[(size_t)row * a.k + tid] : tid == at ? token : -1;
-    if (tid == 0) a.accepted[row] = at;
+}
+
+// CTAs a row: as many as the vocabulary fills (2048 entries each) and as leave every row of the call resident at four CTAs an SM.
+static int verify_cluster(int rows, int V) {
+    int n = 1;
+    while (n < VMAX && n * 2048 < V && (long long)rows * n * 2 <= 4ll * tc_sm_count()) n *= 2;
+    return n;
+}
+
+template <bool LAW16> static csd_status launch_verify(const VerifyArgs& a, int rows, cudaStream_t st) {
+    const int ctas = verify_cluster(rows, a.V);
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)rows * ctas); cfg.blockDim = dim3(32 * VW); cfg.stream = st;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)ctas; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    CSD_CUDA(cudaLaunchKernelEx(&cfg, verify_kernel<LAW16>, a));
+    count_launch();
+    return CSD_OK;
 }
 
 }  // namespace csd
@@ -91,16 +252,12 @@ using namespace csd;
 extern "C" csd_status csd_spec_verify(const void* target_probs_dev, int64_t ld_p, const void* draft_probs_dev, int64_t ld_q, int prob_type,
                                       const int32_t* draft_tokens_dev, const int32_t* n_drafts_dev, const float* uniforms_dev, int rows,
                                       int k, int V, int32_t* n_accepted_dev, int32_t* tokens_dev, void* stream) {
-    if (rows < 0 || k < 0 || k > 64 || V < 1 || (prob_type != CSD_F32 && prob_type != CSD_BF16)) return CSD_ERR_INVALID_ARG;
+    if (rows < 0 || rows > 1 << 24 || k < 0 || k > 64 || V < 1 || (prob_type != CSD_F32 && prob_type != CSD_BF16)) return CSD_ERR_INVALID_ARG;
     if (rows == 0) return CSD_OK;
     if (!target_probs_dev || (k > 0 && !draft_tokens_dev) || !uniforms_dev || !n_accepted_dev || !tokens_dev) return CSD_ERR_INVALID_ARG;
     if (ld_p < V || (draft_probs_dev && ld_q < V)) return CSD_ERR_INVALID_ARG;
     VerifyArgs a{target_probs_dev, draft_probs_dev, draft_tokens_dev, n_drafts_dev, uniforms_dev, n_accepted_dev, tokens_dev,
                  status_word_device(), ld_p, ld_q, k, V};
     if (!a.status) return CSD_ERR_CUDA;
-    if (prob_type == CSD_BF16) verify_kernel<true><<<rows, VT, 0, (cudaStream_t)stream>>>(a);
-    else verify_kernel<false><<<rows, VT, 0, (cudaStream_t)stream>>>(a);
-    CSD_CUDA(cudaGetLastError());
-    count_launch();
-    return CSD_OK;
+    return prob_type == CSD_BF16 ? launch_verify<true>(a, rows, (cudaStream_t)stream) : launch_verify<false>(a, rows, (cudaStream_t)stream);
 }
