@@ -334,22 +334,13 @@ def csd_spec_accept_static(target_logits: torch.Tensor, draft_logits: Optional[t
 ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _on(device: torch.device):
-    """The device's current stream, and the device made current for the call where it is not."""
-    index = device.index
-    if index == torch.cuda.current_device():
-        return torch._C._cuda_getCurrentRawStream(index), None
-    return torch.cuda.current_stream(index).cuda_stream, torch.cuda.device(index)
-
-
-def _call(name: str, fn, device: torch.device, *args) -> None:
-    """fn(*args, stream) on the tensors' device."""
-    stream, guard = _on(device)
-    if guard is None:
-        code = fn(*args, stream)
+def _call(name: str, fn, index: int, *args) -> None:
+    """fn(*args, stream) on the current stream of the tensors' device, made current for the call where it is not."""
+    if index == torch._C._cuda_getDevice():
+        code = fn(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
-        with guard:
-            code = fn(*args, stream)
+        with torch.cuda.device(index):
+            code = fn(*args, torch._C._cuda_getCurrentRawStream(index))
     if code:
         raise CsdError(name, code)
 
@@ -361,16 +352,18 @@ def csd_spec_verify(target_probs: torch.Tensor, draft_probs: Optional[torch.Tens
     each).  Laws may lie further apart than V (a view of a padded vocabulary).  Returns (n_accepted [rows], tokens
     [rows, k+1]: the accepted drafts, the output token, -1 behind it), int32."""
     rows, k1, V = target_probs.shape
-    k, dev = k1 - 1, target_probs.device
+    k, dev = k1 - 1, target_probs.get_device()
     ld_p, ld_q = _law_stride(target_probs), 0
     if draft_probs is not None:
-        assert draft_probs.dtype == target_probs.dtype and tuple(draft_probs.shape) == (rows, k, V) and draft_probs.device == dev
+        assert draft_probs.dtype == target_probs.dtype and draft_probs.shape == (rows, k, V) and draft_probs.get_device() == dev
         ld_q = _law_stride(draft_probs) if k else V
-    assert draft_tokens.dtype == torch.int32 and draft_tokens.is_contiguous() and tuple(draft_tokens.shape) == (rows, k)
-    assert uniforms.dtype == torch.float32 and uniforms.is_contiguous() and tuple(uniforms.shape) == (rows, k1)
-    assert n_drafts is None or (n_drafts.dtype == torch.int32 and n_drafts.is_contiguous() and n_drafts.numel() == rows)
+    assert draft_tokens.dtype == torch.int32 and draft_tokens.is_contiguous() and draft_tokens.shape == (rows, k) and draft_tokens.get_device() == dev
+    assert uniforms.dtype == torch.float32 and uniforms.is_contiguous() and uniforms.shape == (rows, k1) and uniforms.get_device() == dev
+    assert n_drafts is None or (n_drafts.dtype == torch.int32 and n_drafts.is_contiguous() and n_drafts.numel() == rows and n_drafts.get_device() == dev)
     if out is None:
-        out = (torch.empty(rows, dtype=torch.int32, device=dev), torch.empty(rows, k1, dtype=torch.int32, device=dev))
+        out = (draft_tokens.new_empty(rows), draft_tokens.new_empty((rows, k1)))
+    for o, shape in zip(out, ((rows,), (rows, k1))):
+        assert o.dtype == torch.int32 and o.is_contiguous() and o.shape == shape and o.get_device() == dev
     _call("csd_spec_verify", lib.csd_spec_verify, dev, target_probs.data_ptr(), ld_p, _ptr(draft_probs), ld_q, ROW_TYPES[target_probs.dtype],
           draft_tokens.data_ptr(), _ptr(n_drafts), uniforms.data_ptr(), rows, k, V, out[0].data_ptr(), out[1].data_ptr())
     return out
@@ -396,7 +389,7 @@ class KvPool:
             assert k.dtype == torch.float8_e4m3fn
             for e in (k_exp, v_exp):
                 assert e.dtype == torch.uint8 and tuple(e.shape) == (n, H, P) and e.is_contiguous() and e.device == k.device
-        self.k, self.v, self.k_exp, self.v_exp, self.device, self.heads, self.d_head = k, v, k_exp, v_exp, k.device, H, D
+        self.k, self.v, self.k_exp, self.v_exp, self.index, self.heads, self.d_head = k, v, k_exp, v_exp, k.get_device(), H, D
         self.c = KvPoolStruct(int(k.dtype != torch.bfloat16), n, P, H, D, _ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp))
         self.ref = C.addressof(self.c)
 
@@ -419,38 +412,39 @@ class PagedBatch:
             assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.device == page_table.device
         assert row_start.numel() == n + 1 and kv_len.numel() == n
         self.page_table, self.row_start, self.kv_len, self.total_rows, self.max_rows = page_table, row_start, kv_len, total_rows, max_rows
+        self.index = page_table.get_device()
         self.c = PagedBatchStruct(n, pages, total_rows, max_rows, _ptr(page_table), _ptr(row_start), _ptr(kv_len))
         self.ref = C.addressof(self.c)
 
 
-def _row_stride(t: torch.Tensor, batch: PagedBatch, heads: Optional[int], d_head: int, device: torch.device) -> int:
-    """Elements between the rows of [total_rows, heads, d_head], whose heads lie side by side."""
-    assert t.device == device and t.shape[0] == batch.total_rows and t.shape[2] == d_head and (heads is None or t.shape[1] == heads)
+def _row_stride(t: torch.Tensor, rows: int, heads: int, d_head: int, index: int) -> int:
+    """Elements between the rows of [rows, heads, d_head], whose heads lie side by side."""
     a, b, one = t.stride()
-    assert one == 1 and (t.shape[1] == 1 or b == d_head)
-    return a if t.shape[0] > 1 else t.shape[1] * d_head
+    assert t.shape == (rows, heads, d_head) and one == 1 and (b == d_head or heads == 1) and t.get_device() == index
+    return a if rows > 1 else heads * d_head
 
 
 def csd_paged_append(pool: KvPool, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor) -> None:
     """Writes rows k and v [total_rows, n_kv_heads, d_head] (float32 or bfloat16) to the batch's positions of the pool."""
-    ld = _row_stride(k, batch, pool.heads, pool.d_head, pool.device)
-    assert k.dtype == v.dtype and _row_stride(v, batch, pool.heads, pool.d_head, pool.device) == ld
-    _call("csd_paged_append", lib.csd_paged_append, pool.device, pool.ref, batch.ref, k.data_ptr(), v.data_ptr(), ld, ROW_TYPES[k.dtype])
+    ld = _row_stride(k, batch.total_rows, pool.heads, pool.d_head, pool.index)
+    assert k.dtype == v.dtype and batch.index == pool.index and _row_stride(v, batch.total_rows, pool.heads, pool.d_head, pool.index) == ld
+    _call("csd_paged_append", lib.csd_paged_append, pool.index, pool.ref, batch.ref, k.data_ptr(), v.data_ptr(), ld, ROW_TYPES[k.dtype])
 
 
 def csd_paged_read(pool: KvPool, batch: PagedBatch, dtype: torch.dtype = torch.bfloat16, out: Optional[Sequence[torch.Tensor]] = None):
     """The values that the pool holds at the batch's positions: (k, v), each [total_rows, n_kv_heads, d_head]."""
     if out is None:
-        out = tuple(torch.empty(batch.total_rows, pool.heads, pool.d_head, dtype=dtype, device=pool.device) for _ in range(2))
+        k = batch.row_start.new_empty((batch.total_rows, pool.heads, pool.d_head), dtype=dtype)
+        out = k, torch.empty_like(k)
     k, v = out
-    ld = _row_stride(k, batch, pool.heads, pool.d_head, pool.device)
-    assert k.dtype == v.dtype and _row_stride(v, batch, pool.heads, pool.d_head, pool.device) == ld
-    _call("csd_paged_read", lib.csd_paged_read, pool.device, pool.ref, batch.ref, k.data_ptr(), v.data_ptr(), ld, ROW_TYPES[k.dtype])
+    ld = _row_stride(k, batch.total_rows, pool.heads, pool.d_head, pool.index)
+    assert k.dtype == v.dtype and batch.index == pool.index and _row_stride(v, batch.total_rows, pool.heads, pool.d_head, pool.index) == ld
+    _call("csd_paged_read", lib.csd_paged_read, pool.index, pool.ref, batch.ref, k.data_ptr(), v.data_ptr(), ld, ROW_TYPES[k.dtype])
     return out
 
 
 def csd_paged_attention_workspace(pool: KvPool, batch: PagedBatch, n_heads: int, dtype: torch.dtype) -> torch.Tensor:
-    return _ws(lib.csd_paged_attention_workspace_bytes(pool.ref, batch.ref, n_heads, ROW_TYPES[dtype]), pool.device)
+    return _ws(lib.csd_paged_attention_workspace_bytes(pool.ref, batch.ref, n_heads, ROW_TYPES[dtype]), pool.k.device)
 
 
 def csd_paged_attention(q: torch.Tensor, pool: KvPool, batch: PagedBatch, scale: Optional[float] = None,
@@ -459,18 +453,22 @@ def csd_paged_attention(q: torch.Tensor, pool: KvPool, batch: PagedBatch, scale:
     """Attention of rows q [total_rows, n_heads, d_head] (float32 or bfloat16) over the pool, which holds the rows' own keys
     already.  scale None: 1 / sqrt(d_head); tree_mask [total_rows] int64 (bit j: sees row j of its chunk) instead of causal.
     A workspace is zero before its first call and not shared by calls that may overlap."""
-    heads, D = q.shape[1], pool.d_head
-    ldq = _row_stride(q, batch, None, D, pool.device)
+    heads, D, rows, index = q.shape[1], pool.d_head, batch.total_rows, pool.index
+    ldq = _row_stride(q, rows, heads, D, index)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    assert out.dtype == q.dtype and out.shape == q.shape
+        out, ldo = q.new_empty((rows, heads, D)), heads * D
+    else:
+        ldo = _row_stride(out, rows, heads, D, index)
+        assert out.dtype == q.dtype
     if workspace is None:
         workspace = csd_paged_attention_workspace(pool, batch, heads, q.dtype)
+    assert batch.index == index and workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.get_device() == index
+    mask = None
     if tree_mask is not None:
-        assert tree_mask.dtype == torch.int64 and tree_mask.is_contiguous() and tree_mask.numel() == batch.total_rows and tree_mask.device == q.device
-    _call("csd_paged_attention", lib.csd_paged_attention, pool.device, pool.ref, batch.ref, q.data_ptr(), ldq, heads, ROW_TYPES[q.dtype],
-          D ** -0.5 if scale is None else scale, _ptr(tree_mask), out.data_ptr(), _row_stride(out, batch, heads, D, pool.device),
-          workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        assert tree_mask.dtype == torch.int64 and tree_mask.is_contiguous() and tree_mask.numel() == rows and tree_mask.get_device() == index
+        mask = tree_mask.data_ptr()
+    _call("csd_paged_attention", lib.csd_paged_attention, index, pool.ref, batch.ref, q.data_ptr(), ldq, heads, ROW_TYPES[q.dtype],
+          D ** -0.5 if scale is None else scale, mask, out.data_ptr(), ldo, workspace.data_ptr(), workspace.numel())
     return out
 
 
