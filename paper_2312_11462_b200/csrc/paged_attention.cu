@@ -17,10 +17,15 @@ static int packed_rows(const csd_paged_batch* batch, const csd_kv_pool* pool, in
     return n > 1 << 30 ? 1 << 30 : (int)n;
 }
 
+static bool takes_chunks(int packed, int row_type) { return row_type == CSD_BF16 && packed > 32; }
+
 extern "C" size_t csd_paged_attention_workspace_bytes(const csd_kv_pool* pool, const csd_paged_batch* batch, int n_heads, int row_type) {
     PagedView w;
     if (check_attend(pool, batch, n_heads, row_type, &w) != CSD_OK) return 0;
-    return paged_rows_workspace(pool->d_head, packed_rows(batch, pool, n_heads), row_type, w.k_exp != nullptr);
+    // (the call's scale and masks are not known here: room for either kernel)
+    const int packed = packed_rows(batch, pool, n_heads);
+    const size_t rows = paged_rows_workspace(pool->d_head, packed, row_type, w.k_exp != nullptr), chunk = paged_chunk_workspace(pool->d_head);
+    return takes_chunks(packed, row_type) && chunk > rows ? chunk : rows;
 }
 
 extern "C" csd_status csd_paged_attention(const csd_kv_pool* pool, const csd_paged_batch* batch, const void* q_dev, int64_t ldq, int n_heads,
@@ -38,5 +43,8 @@ extern "C" csd_status csd_paged_attention(const csd_kv_pool* pool, const csd_pag
     w.status = status_word_device();
     if (!w.status) return CSD_ERR_CUDA;
     AttendArgs a{q_dev, out_dev, (const u64*)tree_mask_dev, ldq, ldo, n_heads / pool->n_kv_heads, scale, nullptr, nullptr};
-    return launch_paged_rows(w, a, pool->d_head, packed_rows(batch, pool, n_heads), row_type, workspace_dev, (cudaStream_t)stream);
+    const int packed = packed_rows(batch, pool, n_heads);
+    if (takes_chunks(packed, row_type) && !tree_mask_dev && scale > 0.f)
+        return launch_paged_chunk(w, a, pool->d_head, workspace_dev, (cudaStream_t)stream);
+    return launch_paged_rows(w, a, pool->d_head, packed, row_type, workspace_dev, (cudaStream_t)stream);
 }

@@ -1,0 +1,525 @@
+// Attention over the paged cache for chunks of many bf16 rows: prompts, and the chunks of long ones.
+//
+// What bounds it are the products, 4 d flops a (row, key, head), and the exponentials beside them.  A CTA takes blocks of 256 (row, query head)
+// pairs, two accumulator halves of 128 rows, against tiles of 128 positions.  Warps 0-3 load: pages are gathered with cp.async into
+// 128-byte-swizzled tiles, 8-bit rows are widened to bf16 on the way (value times scale is exact there).  Warp 12 issues
+// tcgen05.mma: scores S = Q K^T from shared memory, output O += P V with P from tensor memory.  Warps 4-7 and 8-11 take a half each, a
+// thread a row: running maximum, exponentials, P as bf16 over the scores' columns.  The two halves alternate, so that one's products run
+// under the other's exponentials.  The output stays in tensor memory; it is rescaled only when a maximum has grown by more than 2^8.
+//
+// All products of a CTA are issued by one thread and run in order: when S of tile t + 1 is there, O += P V of tile t is done, so a
+// softmax thread may rescale O without another barrier, and S may overwrite the P that the product before it has read.
+#include "paged_attention.cuh"
+#include "tc_common.cuh"
+
+namespace csd {
+
+constexpr int CH_KEYS = 128, CH_ROWS = 256, CH_THREADS = 13 * 32;
+constexpr float CH_LATE = 8.f;                  // a running maximum may lag by this power of two
+
+template <int DH> struct ChunkCfg {
+    static constexpr int HALVES = DH / 64;                       // 64-column halves of a row, 128 bytes each
+    static constexpr int TILE_BYTES = CH_KEYS * DH * 2;          // a tile of keys or of values
+    static constexpr int SLOTS = DH == 128 ? 5 : 8;
+    static constexpr int Q_BYTES = CH_ROWS * DH * 2;
+    static constexpr int SMEM = 1024 + Q_BYTES + SLOTS * TILE_BYTES;
+    static constexpr int PART = CH_ROWS * (DH + 2);              // floats of a part: rows, maxima, sums
+    static constexpr int O_COL = 256;                            // tensor memory: S0, S1 (128 columns each), O0, O1
+};
+
+struct ChunkBars {
+    uint64_t full[8], free_[8], qfull, qfree, sfull[2], pready[2], ofull[2], ofree[2], joined[2], told[2];
+    uint32_t tmem;
+    int abort_flag, last[2];
+    unsigned lost[8];                                            // of the run's last eight key tiles: groups of 16 without a page
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+// operand with 64 consecutive elements (of N) per 128-byte row and K down the rows: atoms of 8 rows 1024 bytes apart along K,
+// the next 64 elements `next64` bytes on
+__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t addr, uint32_t next64) {
+    uint64_t d = smem_desc_sw128(addr);
+    d &= ~((uint64_t)0x3fff << 16);
+    return d | (uint64_t)(next64 >> 4) << 16;
+}
+// A from tensor memory
+__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
+    asm volatile("{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
+                 ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accum) : "memory");
+}
+__device__ __forceinline__ void tm_ld32(uint32_t addr, float (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]),
+                   "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]),
+                   "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void tm_st32(uint32_t addr, const float (&v)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+                 ::"f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]),
+                   "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]),
+                   "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t (&v)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+                   "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// four e4m3 numbers times 2^120 * one (two bf16 each of `one`: the row's scale), as two words of two bf16
+__device__ __forceinline__ uint2 widen4(uint32_t w, uint32_t one) {
+    w = __byte_perm(w, 0, 0x3120);                               // numbers 0, 2, 1, 3
+    uint32_t a = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u), b = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
+    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(0x7b807b80u));
+    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(b) : "r"(0x7b807b80u));
+    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(one));
+    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(b) : "r"(one));
+    return make_uint2(a, b);
+}
+
+// byte offset of 16-byte chunk c of row r in a tile of `rows` rows: 64-column halves one behind the other, 128-byte swizzle
+__device__ __forceinline__ uint32_t tile_off(int r, int c, int rows) { return (uint32_t)((c >> 3) * (rows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
+
+typedef Schedule<CH_ROWS, CH_KEYS> ChunkSchedule;
+
+// What a run has of an item, and the halves' own ends.
+struct ChunkPiece {
+    int first, stop, p0, nrows, end[2], see[2];                  // see: positions that all rows of the half see
+    bool whole;
+    __device__ __forceinline__ ChunkPiece(const PagedView& w, const ChunkSchedule::Cursor& at, u64 run_end, int group) {
+        const u64 item_end = at.item_first + at.tiles;
+        first = at.tile;
+        stop = (int)((item_end < run_end ? item_end : run_end) - at.item_first);
+        whole = first == 0 && item_end <= run_end;
+        p0 = at.rb * CH_ROWS;
+        nrows = min(CH_ROWS, at.q.rows * group - p0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int last = min(at.q.rows - 1, (p0 + 128 * i + 127) / group);
+            const int tiles = nrows > 128 * i ? (min(at.q.kv + last + 1, w.capacity) + CH_KEYS - 1) / CH_KEYS : 0;
+            end[i] = min(stop, tiles);
+            see[i] = min(at.q.kv + (p0 + 128 * i) / group + 1, w.capacity);
+        }
+    }
+};
+
+template <int DH, bool E4M3>
+__global__ void __launch_bounds__(CH_THREADS, 1)
+paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
+    using C = ChunkCfg<DH>;
+    extern __shared__ unsigned char smem_dyn[];
+    __shared__ ChunkBars bars;
+    unsigned char* Qs = (unsigned char*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
+    unsigned char* slots = Qs + C::Q_BYTES;
+    u64* prefix = reinterpret_cast<u64*>(Qs);                    // (until the run's first unit is found)
+    static_assert((CSD_MAX_SEQS + 1) * 8 <= C::Q_BYTES, "the prefix fits");
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, group = a.group;
+
+    pdl_wait();
+    ChunkSchedule::count<CH_THREADS>(w, group, false, prefix);
+    const u64 units = prefix[w.n_seqs], most = units / (unsigned)least_units;
+    const unsigned n_runs = most < 1 ? 1u : most < gridDim.x ? (unsigned)most : gridDim.x;
+    if (blockIdx.x >= n_runs || units == 0) return;
+    const u64 begin = run_begin(blockIdx.x, units, n_runs), end = run_begin(blockIdx.x + 1, units, n_runs);
+
+    if (tid == 0) {
+        for (int i = 0; i < 8; ++i) { mbar_init(&bars.full[i], 4); mbar_init(&bars.free_[i], 1); }
+        mbar_init(&bars.qfull, 4); mbar_init(&bars.qfree, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars.sfull[i], 1); mbar_init(&bars.pready[i], 4); mbar_init(&bars.ofull[i], 1); mbar_init(&bars.ofree[i], 4);
+            mbar_init(&bars.joined[i], 4); mbar_init(&bars.told[i], 1);
+        }
+        bars.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 12) {
+        // behind the dependency wait: a kernel before this one may hold tensor memory until it ends
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    ChunkSchedule::Cursor at;
+    at.seek(w, prefix, begin, group, false);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars.tmem;
+    volatile int* gave_up = &bars.abort_flag;
+    pdl_trigger();
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (*gave_up) return false;
+        if (mbar_wait(bar, parity)) return true;
+        *gave_up = 1;
+        return false;
+    };
+    auto warp_waits = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+
+    u64 unit = begin;
+    auto advance = [&](const ChunkPiece& p) {
+        unit = at.item_first + p.stop;
+        if (unit < end) { at.tile = p.stop - 1; at.next(w, group, false); }
+    };
+
+    if (warp < 4) {
+        // ---- loaders.  Tiles in the order K, V of a position tile; each is announced two tiles later, when its copies have landed
+        unsigned n = 0;                                          // tiles so far
+        int pieces = 0;
+        uint64_t* waiting[2] = {nullptr, nullptr};               // barriers of the groups in flight, oldest first
+        auto announce = [&](uint64_t* bar) {
+            if (!bar) return;
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        };
+        auto in_flight = [&](uint64_t* bar) {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group 2;" ::: "memory");
+            announce(waiting[0]);
+            waiting[0] = waiting[1]; waiting[1] = bar; 
+        };
+        bool ok = true;
+        while (unit < end && ok) {
+            const ChunkPiece p(w, at, end, group);
+            if (pieces > 0) {                                    // (the item before needs all its tiles to leave its queries)
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                announce(waiting[0]);
+                announce(waiting[1]);
+                waiting[0] = waiting[1] = nullptr;
+            }
+            if (pieces > 0) ok = warp_waits(&bars.qfree, (uint32_t)(pieces - 1) & 1u);
+            if (!ok) break;
+            for (int i = tid; i < CH_ROWS * (DH / 8); i += 128) {
+                const int r = i / (DH / 8), c = i % (DH / 8), pr = p.p0 + r;
+                const bool there = r < p.nrows;
+                const size_t src = there ? (size_t)(at.q.start + pr / group) * a.ldq + (size_t)(at.h * group + pr % group) * DH + 8 * c : 0;
+                cp_async16(smem_u32(Qs) + (r >> 7) * (128 * DH * 2) + tile_off(r & 127, c, 128), (const uint16_t*)a.q + src, there);
+            }
+            in_flight(&bars.qfull);
+            ++pieces;
+            for (int t = p.first; t < p.stop && ok; ++t) {
+                const int t0 = t * CH_KEYS, left = at.seen - t0;
+                // pages of the tile's eight groups of 16
+                int page = -1;
+                if (lane < 8 && 16 * lane < left) page = paged_page(w, at.s, t0 + 16 * lane);
+                const unsigned lost = __ballot_sync(0xffffffffu, lane < 8 && 16 * lane < left && page < 0);
+                if (tid == 0) bars.lost[n >> 1 & 7] = lost;
+#pragma unroll 1
+                for (int kv = 0; kv < 2 && ok; ++kv, ++n) {
+                    const int slot = (int)(n % C::SLOTS);
+                    if (n >= (unsigned)C::SLOTS) ok = warp_waits(&bars.free_[slot], (n / C::SLOTS - 1) & 1u);
+                    if (!ok) break;
+                    const uint32_t dst = smem_u32(slots) + slot * C::TILE_BYTES;
+                    const unsigned char* pool = kv ? w.v : w.k;
+                    if constexpr (!E4M3) {
+                        constexpr int PER = DH / 8;              // 16-byte chunks of a row
+#pragma unroll
+                        for (int i = 0; i < CH_KEYS * PER / 128; ++i) {
+                            const int key = (i * 128 + tid) / PER, c = tid % PER;
+                            const int pg = __shfl_sync(0xffffffffu, page, key >> 4);
+                            const bool there = pg >= 0 && key < left;
+                            const size_t row = there ? paged_row(w, pg, at.h, t0 + key) : 0;
+                            cp_async16(dst + tile_off(key, c, CH_KEYS), pool + (row * DH + 8 * c) * 2, there);
+                        }
+                    } else {
+                        constexpr int PER = DH / 16, N = CH_KEYS * PER / 128;
+                        uint4 raw[N];
+                        unsigned e[N];
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const int key = (i * 128 + tid) / PER, c = tid % PER;
+                            const int pg = __shfl_sync(0xffffffffu, page, key >> 4);
+                            const bool there = pg >= 0 && key < left;
+                            const size_t row = there ? paged_row(w, pg, at.h, t0 + key) : 0;
+                            raw[i] = there ? *reinterpret_cast<const uint4*>(pool + row * DH + 16 * c) : make_uint4(0u, 0u, 0u, 0u);
+                            e[i] = there ? (kv ? w.v_exp : w.k_exp)[row] : 127u;
+                        }
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const int key = (i * 128 + tid) / PER, c = tid % PER;
+                            const uint32_t one = pack_bf16(row_scale(e[i]), row_scale(e[i]));
+                            const uint2 x = widen4(raw[i].x, one), y = widen4(raw[i].y, one), z = widen4(raw[i].z, one), u = widen4(raw[i].w, one);
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + tile_off(key, 2 * c, CH_KEYS)), "r"(x.x), "r"(x.y), "r"(y.x), "r"(y.y) : "memory");
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + tile_off(key, 2 * c + 1, CH_KEYS)), "r"(z.x), "r"(z.y), "r"(u.x), "r"(u.y) : "memory");
+                        }
+                    }
+                    in_flight(&bars.full[slot]);
+                }
+            }
+            advance(p);
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        announce(waiting[0]);
+        announce(waiting[1]);
+    } else if (warp == 12) {
+        // ---- products
+        if (lane == 0) {
+            constexpr uint32_t F = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);      // bf16 x bf16 -> fp32, 128 rows
+            constexpr uint32_t IDESC_S = F | ((uint32_t)(CH_KEYS >> 3) << 17), IDESC_O = F | (1u << 16) | ((uint32_t)(DH >> 3) << 17);   // (V: N along the rows)
+            const uint64_t qd = smem_desc_sw128(smem_u32(Qs)), kd = smem_desc_sw128(smem_u32(slots)), vd = smem_desc_sw128_mn(smem_u32(slots), CH_KEYS * 128);
+            unsigned n = 0;                                      // tile of the K of the piece's first position tile
+            int pieces = 0, rounds[2] = {0, 0};                  // pieces that a half had tiles of
+            uint32_t tiles_done[2] = {0, 0};
+            bool ok = true;
+            auto scores = [&](int i, unsigned tile) {
+                const uint64_t q = qd + (uint64_t)((i * 128 * DH * 2) >> 4), k = kd + (uint64_t)((tile % C::SLOTS * C::TILE_BYTES) >> 4);
+#pragma unroll
+                for (int ks = 0; ks < DH / 16; ++ks) {
+                    const uint32_t off = (uint32_t)((ks >> 2) * (128 * 128) + (ks & 3) * 32) >> 4;
+                    tc_mma(tmem + 128 * i, q + off, k + off, IDESC_S, ks > 0);
+                }
+                tc_commit(&bars.sfull[i]);
+            };
+            while (unit < end && ok) {
+                const ChunkPiece p(w, at, end, group);
+                ok = wait(&bars.qfull, (uint32_t)pieces & 1u);
+                if (ok) ok = wait(&bars.full[n % C::SLOTS], (n / C::SLOTS) & 1u);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (p.first < p.end[i]) scores(i, n);
+                tc_commit(&bars.free_[n % C::SLOTS]);
+                if (p.stop == p.first + 1) tc_commit(&bars.qfree);
+                for (int t = p.first; t < p.stop && ok; ++t, n += 2) {
+                    const unsigned v = n + 1, k = n + 2;
+                    const bool more = t + 1 < p.stop;
+                    ok = wait(&bars.full[v % C::SLOTS], (v / C::SLOTS) & 1u);
+                    if (ok && more) ok = wait(&bars.full[k % C::SLOTS], (k / C::SLOTS) & 1u);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (!ok || t >= p.end[i]) continue;
+                        if (t == p.first && rounds[i] > 0) ok = wait(&bars.ofree[i], (uint32_t)(rounds[i] - 1) & 1u);
+                        if (ok) ok = wait(&bars.pready[i], tiles_done[i] & 1u);
+                        if (!ok) continue;
+                        ++tiles_done[i];
+                        tc_fence_after();
+                        const uint64_t vt = vd + (uint64_t)((v % C::SLOTS * C::TILE_BYTES) >> 4);
+#pragma unroll
+                        for (int ks = 0; ks < CH_KEYS / 16; ++ks)
+                            tc_mma_ts(tmem + C::O_COL + 128 * i, tmem + 128 * i + 8 * ks, vt + (uint64_t)((ks * 2048) >> 4), IDESC_O, t > p.first || ks > 0);
+                        if (t + 1 == p.end[i]) { tc_commit(&bars.ofull[i]); ++rounds[i]; }
+                        if (t + 1 < p.end[i]) scores(i, k);
+                    }
+                    if (!ok) break;
+                    tc_commit(&bars.free_[v % C::SLOTS]);
+                    if (more) tc_commit(&bars.free_[k % C::SLOTS]);
+                    if (t + 2 == p.stop) tc_commit(&bars.qfree);
+                }
+                ++pieces;
+                advance(p);
+            }
+        }
+    } else {
+        // ---- softmax: a half of the block's rows, a thread a row
+        const int half = (warp - 4) >> 2, quad = warp & 3, r = 128 * half + 32 * quad + lane;
+        const uint32_t lanes = (uint32_t)(32 * quad) << 16, S = tmem + lanes + 128 * half, O = tmem + lanes + C::O_COL + 128 * half;
+        const float to_log2 = a.scale * 1.4426950408889634f;
+        uint32_t tiles_done = 0, run_tiles = 0, joins = 0;
+        int rounds = 0;
+        bool ok = true;
+        while (unit < end && ok) {
+            const ChunkPiece p(w, at, end, group);
+            const int p_row = p.p0 + r, token = p_row / group;
+            const bool mine = r < p.nrows;
+            const int lim = mine ? min(at.q.kv + token + 1, w.capacity) : 0;
+            float m = -INFINITY, l = 0.f;
+            for (int t = p.first; t < p.end[half] && ok; ++t) {
+                ok = warp_waits(&bars.sfull[half], tiles_done & 1u);
+                if (!ok) break;
+                ++tiles_done;
+                tc_fence_after();
+                const unsigned lost = bars.lost[(run_tiles + (t - p.first)) & 7];
+                const int sees = lim - t * CH_KEYS;              // of the tile's positions
+                const bool edge = (t + 1) * CH_KEYS > p.see[half] || lost != 0;
+                auto mask = [&](float (&x)[32], int j0) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j0 + j >= sees || (lost >> ((j0 + j) >> 4) & 1)) x[j] = -INFINITY;
+                };
+                float x[32], y[32];
+                tm_ld32(S + 64, x);
+                tm_ld32(S + 96, y);
+                tm_wait_ld();
+                if (edge) { mask(x, 64); mask(y, 96); }
+                float top = fmaxf(x[0], y[0]);
+#pragma unroll
+                for (int j = 1; j < 32; ++j) top = fmaxf(top, fmaxf(x[j], y[j]));
+                tm_ld32(S, x);
+                tm_ld32(S + 32, y);
+                tm_wait_ld();
+                if (edge) { mask(x, 0); mask(y, 32); }
+#pragma unroll
+                for (int j = 0; j < 32; ++j) top = fmaxf(top, fmaxf(x[j], y[j]));
+                top *= to_log2;                                  // (the scale is positive here)
+                if (__any_sync(0xffffffffu, top > m + CH_LATE)) {
+                    const float nm = fmaxf(m, top), keep = nm == -INFINITY ? 0.f : ex2(m - nm);
+                    m = nm;
+                    l *= keep;
+                    if (t > p.first) {
+                        float o[32];
+#pragma unroll 1
+                        for (int c = 0; c < DH; c += 32) {
+                            tm_ld32(O + c, o);
+                            tm_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) o[j] *= keep;
+                            tm_st32(O + c, o);
+                        }
+                    }
+                }
+                const float base = m == -INFINITY ? 0.f : m;
+                float sum = 0.f, sum2 = 0.f;
+                auto weights = [&](float (&s)[32], int col) {
+                    uint32_t u[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const float e0 = ex2(fmaf(s[2 * j], to_log2, -base)), e1 = ex2(fmaf(s[2 * j + 1], to_log2, -base));
+                        sum += e0; sum2 += e1;
+                        u[j] = pack_bf16(e0, e1);
+                    }
+                    tm_st16(S + col, u);
+                };
+                weights(x, 0);
+                weights(y, 16);
+                tm_ld32(S + 64, x);
+                tm_ld32(S + 96, y);
+                tm_wait_ld();
+                if (edge) { mask(x, 64); mask(y, 96); }
+                weights(x, 32);
+                weights(y, 48);
+                l += sum + sum2;
+                tm_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.pready[half]);
+            }
+            if (!ok) break;
+            // ---- the rows leave, finished or as a part of their item
+            const bool any = p.first < p.end[half];
+            if (any) {
+                ok = warp_waits(&bars.ofull[half], (uint32_t)rounds & 1u);
+                if (!ok) break;
+                ++rounds;
+                tc_fence_after();
+            }
+            float* part = a.parts + ((size_t)blockIdx.x * 2 + (p.first == 0 ? 1 : 0)) * C::PART;
+            const size_t dst = mine ? (size_t)(at.q.start + token) * a.ldo + (size_t)(at.h * group + p_row % group) * DH : 0;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            if (any) {
+#pragma unroll 1
+                for (int c = 0; c < DH; c += 32) {
+                    float o[32];
+                    tm_ld32(O + c, o);
+                    tm_wait_ld();
+                    if (!mine) continue;
+                    if (p.whole) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8)
+                            *reinterpret_cast<uint4*>((uint16_t*)a.out + dst + c + j) =
+                                make_uint4(pack_bf16(o[j] * inv, o[j + 1] * inv), pack_bf16(o[j + 2] * inv, o[j + 3] * inv),
+                                           pack_bf16(o[j + 4] * inv, o[j + 5] * inv), pack_bf16(o[j + 6] * inv, o[j + 7] * inv));
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4)
+                            __stcg(reinterpret_cast<float4*>(part + (size_t)r * DH + c + j), make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.ofree[half]);
+            }
+            if (!p.whole && p.nrows > 128 * half) {
+                if (mine) { __stcg(part + CH_ROWS * DH + r, m); __stcg(part + CH_ROWS * DH + CH_ROWS + r, l); }
+                // the half's last part to arrive adds them up, in the order of their runs
+                const int c0 = run_of(at.item_first, units, n_runs), c1 = run_of(at.item_first + at.tiles - 1, units, n_runs);
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars.joined[half]);
+                if (quad == 0) {
+                    ok = warp_waits(&bars.joined[half], joins & 1u);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        bars.last[half] = atomicInc(a.tickets + 2 * c0 + half, (unsigned)(c1 - c0)) == (unsigned)(c1 - c0);
+                        mbar_arrive(&bars.told[half]);
+                    }
+                }
+                ok = warp_waits(&bars.told[half], joins++ & 1u);
+                if (!ok) break;
+                if (bars.last[half]) {
+                    __threadfence();
+                    auto of = [&](int c) { return a.parts + ((size_t)c * 2 + (c == c0 ? 1 : 0)) * C::PART; };
+                    float top = -INFINITY, total = 0.f;
+                    if (mine) {
+                        for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(of(c) + CH_ROWS * DH + r));
+                        const float base = top == -INFINITY ? 0.f : top;
+                        for (int c = c0; c <= c1; ++c) total += ex2(__ldcg(of(c) + CH_ROWS * DH + r) - base) * __ldcg(of(c) + CH_ROWS * DH + CH_ROWS + r);
+                        top = base;
+                    }
+                    const float scale = total == 0.f ? 0.f : 1.f / total;
+                    // a warp its 32 rows, lanes along a row
+                    constexpr int PER = DH / 4;
+                    for (int i = lane; i < 32 * PER; i += 32) {
+                        const int rr = i / PER, row = 128 * half + 32 * quad + rr, d = i % PER * 4;
+                        const float row_top = __shfl_sync(0xffffffffu, top, rr), row_scale_ = __shfl_sync(0xffffffffu, scale, rr);
+                        if (row >= p.nrows) continue;
+                        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int c = c0; c <= c1; ++c) {
+                            const float pm = __ldcg(of(c) + CH_ROWS * DH + row);
+                            if (pm == -INFINITY) continue;       // (nothing was written of the rows)
+                            const float f = ex2(pm - row_top);
+                            const float4 x = __ldcg(reinterpret_cast<const float4*>(of(c) + (size_t)row * DH + d));
+                            v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
+                        }
+                        const int pp = p.p0 + row;
+                        const size_t to = (size_t)(at.q.start + pp / group) * a.ldo + (size_t)(at.h * group + pp % group) * DH + d;
+                        *reinterpret_cast<uint2*>((uint16_t*)a.out + to) =
+                            make_uint2(pack_bf16(v.x * row_scale_, v.y * row_scale_), pack_bf16(v.z * row_scale_, v.w * row_scale_));
+                    }
+                }
+            }
+            run_tiles += (uint32_t)(p.stop - p.first);
+            advance(p);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (*gave_up) {
+        if (tid == 0) set_status(w.status, CSD_ERR_TIMEOUT);
+        __nanosleep(2000000);                    // let products already issued end before the CTA's memory is released
+    }
+    if (warp == 12) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+template <int DH, bool E4M3> static csd_status run_chunk(const PagedView& w, const AttendArgs& a, cudaStream_t st) {
+    auto kern = paged_chunk_kernel<DH, E4M3>;
+    static PerDevice ready;
+    const csd_status ok = allow_smem(ready, kern, ChunkCfg<DH>::SMEM);
+    if (ok != CSD_OK) return ok;
+    PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(CH_THREADS), ChunkCfg<DH>::SMEM, st);
+    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a, 1));
+    count_launch();
+    return CSD_OK;
+}
+
+size_t paged_chunk_workspace(int d_head) {
+    return PAGED_TICKET_BYTES + (size_t)tc_sm_count() * 2 * (d_head == 64 ? ChunkCfg<64>::PART : ChunkCfg<128>::PART) * 4;
+}
+
+csd_status launch_paged_chunk(const PagedView& w, AttendArgs a, int d_head, void* workspace, cudaStream_t st) {
+    a.tickets = (unsigned*)workspace;
+    a.parts = (float*)((char*)workspace + PAGED_TICKET_BYTES);
+    if (d_head == 64) return w.k_exp ? run_chunk<64, true>(w, a, st) : run_chunk<64, false>(w, a, st);
+    return w.k_exp ? run_chunk<128, true>(w, a, st) : run_chunk<128, false>(w, a, st);
+}
+
+}  // namespace csd

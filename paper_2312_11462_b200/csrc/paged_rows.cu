@@ -520,15 +520,13 @@ struct RowsRun {
     template <int D, int M, bool R, bool E> csd_status operator()() const { return run_rows<D, M, R, E>(w, a, st); }
 };
 
-constexpr size_t TICKET_BYTES = 4096;
-
 size_t paged_rows_workspace(int d_head, int packed_rows, int row_type, bool e4m3) {
-    return TICKET_BYTES + pick_rows(d_head, packed_rows, row_type, e4m3, RowsBytes());
+    return PAGED_TICKET_BYTES + pick_rows(d_head, packed_rows, row_type, e4m3, RowsBytes());
 }
 
 csd_status launch_paged_rows(const PagedView& w, AttendArgs a, int d_head, int packed_rows, int row_type, void* workspace, cudaStream_t st) {
     a.tickets = (unsigned*)workspace;
-    a.parts = (float*)((char*)workspace + TICKET_BYTES);
+    a.parts = (float*)((char*)workspace + PAGED_TICKET_BYTES);
     return pick_rows(d_head, packed_rows, row_type, w.k_exp != nullptr, RowsRun{w, a, st});
 }
 
