@@ -162,10 +162,7 @@ static std::mutex g_map_mu;
 static std::unordered_map<MapKey, CUtensorMap, MapHash> g_maps;
 
 // [rows][K] bf16 row-major, boxes of box_rows x 64 elements, 128-byte swizzle, zero fill outside
-bool tensor_map_2d(const void* W, int N, int K, int box_rows, CUtensorMap* out) {
-    std::lock_guard<std::mutex> lk(g_map_mu);
-    auto it = g_maps.find(MapKey{W, N, K, box_rows});
-    if (it != g_maps.end()) { *out = it->second; return true; }
+bool encode_map_2d(const void* W, int N, int K, int box_rows, CUtensorMap* out) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     CUtensorMap tm;
@@ -177,6 +174,16 @@ bool tensor_map_2d(const void* W, int N, int K, int box_rows, CUtensorMap* out) 
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return false;
+    *out = tm;
+    return true;
+}
+
+bool tensor_map_2d(const void* W, int N, int K, int box_rows, CUtensorMap* out) {
+    std::lock_guard<std::mutex> lk(g_map_mu);
+    auto it = g_maps.find(MapKey{W, N, K, box_rows});
+    if (it != g_maps.end()) { *out = it->second; return true; }
+    CUtensorMap tm;
+    if (!encode_map_2d(W, N, K, box_rows, &tm)) return false;
     if (g_maps.size() > 4096) g_maps.clear();
     g_maps.emplace(MapKey{W, N, K, box_rows}, tm);
     *out = tm;

@@ -6,6 +6,16 @@ namespace csd {
 
 constexpr size_t PAGED_TICKET_BYTES = 4096;      // tickets at the start of the workspace: zero between calls, whatever their shapes
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// whether either of two bf16 is an infinity or NaN
+__device__ __forceinline__ bool odd_bf16(uint32_t two) { return (two & 0x7f80u) == 0x7f80u || (two & 0x7f800000u) == 0x7f800000u; }
+
 // Few rows (decode, reviews, trees) or fp32 rows: paged_rows.cu
 size_t paged_rows_workspace(int d_head, int packed_rows, int row_type, bool e4m3);
 csd_status launch_paged_rows(const PagedView& w, AttendArgs a, int d_head, int packed_rows, int row_type, void* workspace, cudaStream_t st);

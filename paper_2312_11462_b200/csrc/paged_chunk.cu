@@ -1,42 +1,50 @@
 // Attention over the paged cache for chunks of many bf16 rows: prompts, and the chunks of long ones.
 //
 // What bounds it are the products, 4 d flops a (row, key, head), and the exponentials beside them.  A CTA takes blocks of 256 (row, query head)
-// pairs, two accumulator halves of 128 rows, against tiles of 128 positions.  Warps 0-3 load: pages are gathered with cp.async into
-// 128-byte-swizzled tiles, 8-bit rows are widened to bf16 on the way (value times scale is exact there).  Warp 12 issues
-// tcgen05.mma: scores S = Q K^T from shared memory, output O += P V with P from tensor memory.  Warps 4-7 and 8-11 take a half each, a
-// thread a row: running maximum, exponentials, P as bf16 over the scores' columns.  The two halves alternate, so that one's products run
-// under the other's exponentials.  The output stays in tensor memory; it is rescaled only when a maximum has grown by more than 2^8.
+// pairs, two accumulator halves of 128 rows, against tiles of 128 positions, in four groups of four warps:
+//   0  warp 0 requests the pages of a tile by TMA (a box a page and 64 columns; 8-bit pages and their scales as they lie, one copy
+//      each); warp 1 issues tcgen05.mma, scores S = Q K^T from shared memory and output O += P V with P from tensor memory; warps 2 and 3
+//      gather the block's queries
+//   1  widens 8-bit tiles to bf16 (value times scale is exact there), and puts bf16 tiles of values that not every row sees in order
+//   2, 3  a half of the rows each, a thread a row: running maximum, exponentials, P as bf16 over the scores' columns.  The halves alternate,
+//      so that one's products run under the other's exponentials.  They take most of the registers.
+// The output stays in tensor memory; it is rescaled only when a maximum has grown by more than 2^8.
 //
 // All products of a CTA are issued by one thread and run in order: when S of tile t + 1 is there, O += P V of tile t is done, so a
 // softmax thread may rescale O without another barrier, and S may overwrite the P that the product before it has read.
+//
+// What lies behind a sequence's positions may be anything, and 0 x NaN is NaN: values behind the last position are zeroed, and so
+// are infinities and NaN in positions that some of the block's rows do not see; rows that see them get them added at the end.
 #include "paged_attention.cuh"
 #include "tc_common.cuh"
 
 namespace csd {
 
-constexpr int CH_KEYS = 128, CH_ROWS = 256, CH_THREADS = 13 * 32;
+constexpr int CH_KEYS = 128, CH_ROWS = 256, CH_THREADS = 512;
+constexpr int CH_MORE = 168, CH_FEWER = 88;     // registers of a softmax thread and of the others: 512 threads are launched with 128 each
+static_assert(256 * CH_MORE + 256 * CH_FEWER <= 512 * 128, "a setmaxnreg.inc beyond the launch's registers would wait for good");
 constexpr float CH_LATE = 8.f;                  // a running maximum may lag by this power of two
 
-template <int DH> struct ChunkCfg {
+template <int DH, bool E4M3> struct ChunkCfg {
     static constexpr int HALVES = DH / 64;                       // 64-column halves of a row, 128 bytes each
     static constexpr int TILE_BYTES = CH_KEYS * DH * 2;          // a tile of keys or of values
-    static constexpr int SLOTS = DH == 128 ? 5 : 8;
+    static constexpr int SLOTS = DH == 64 ? 8 : E4M3 ? 4 : 5;
+    static constexpr int RAW = E4M3 ? CH_KEYS * DH + CH_KEYS : 0;        // a tile as the pool has it, and its scales
+    static constexpr int RAWS = E4M3 ? 2 : 0;
     static constexpr int Q_BYTES = CH_ROWS * DH * 2;
-    static constexpr int SMEM = 1024 + Q_BYTES + SLOTS * TILE_BYTES;
-    static constexpr int PART = CH_ROWS * (DH + 2);              // floats of a part: rows, maxima, sums
+    static constexpr int SMEM = 1024 + Q_BYTES + SLOTS * TILE_BYTES + RAWS * RAW;
+    static constexpr int PART = CH_ROWS * (DH + 2);              // floats of a part: [half][column][row], maxima, sums
     static constexpr int O_COL = 256;                            // tensor memory: S0, S1 (128 columns each), O0, O1
 };
 
 struct ChunkBars {
-    uint64_t full[8], free_[8], qfull, qfree, sfull[2], pready[2], ofull[2], ofree[2], joined[2], told[2];
+    uint64_t full[8], free_[8], landed[8], rawfull[2], rawfree[2], qfull, qfree, sfull[2], pready[2], ofull[2], ofree[2], joined[2], told[2];
     uint32_t tmem;
     int abort_flag, last[2];
-    unsigned lost[8];                                            // of the run's last eight key tiles: groups of 16 without a page
+    // of the run's last eight position tiles: groups of 16 without a page; positions with values that were taken out
+    unsigned lost[8], odd[8][4];
 };
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
 // operand with 64 consecutive elements (of N) per 128-byte row and K down the rows: atoms of 8 rows 1024 bytes apart along K,
 // the next 64 elements `next64` bytes on
 __device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t addr, uint32_t next64) {
@@ -70,21 +78,25 @@ __device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t (&v)[16]) 
 __device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-// four e4m3 numbers times 2^120 * one (two bf16 each of `one`: the row's scale), as two words of two bf16
-__device__ __forceinline__ uint2 widen4(uint32_t w, uint32_t one) {
+// four e4m3 numbers times a power of two, `up` times `rest` less the 2^120 that the exponent fields lie apart, as two words of two bf16
+__device__ __forceinline__ uint2 widen4(uint32_t w, uint32_t up, uint32_t rest, bool twice) {
     w = __byte_perm(w, 0, 0x3120);                               // numbers 0, 2, 1, 3
     uint32_t a = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u), b = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
-    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(0x7b807b80u));
-    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(b) : "r"(0x7b807b80u));
-    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(one));
-    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(b) : "r"(one));
+    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(up));
+    asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(b) : "r"(up));
+    if (twice) {
+        asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(rest));
+        asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(b) : "r"(rest));
+    }
     return make_uint2(a, b);
 }
-
+// 2^e as two bf16 (a field of 8 exponent bits, e + 127 of 1 .. 254)
+__device__ __forceinline__ uint32_t two_powers(unsigned field) { return field << 7 | field << 23; }
+// copies `bytes` (a multiple of 16) as they lie
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
 // byte offset of 16-byte chunk c of row r in a tile of `rows` rows: 64-column halves one behind the other, 128-byte swizzle
 __device__ __forceinline__ uint32_t tile_off(int r, int c, int rows) { return (uint32_t)((c >> 3) * (rows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 
@@ -113,12 +125,13 @@ struct ChunkPiece {
 
 template <int DH, bool E4M3>
 __global__ void __launch_bounds__(CH_THREADS, 1)
-paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
-    using C = ChunkCfg<DH>;
+paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PagedView w, const AttendArgs a, int least_units) {
+    using C = ChunkCfg<DH, E4M3>;
     extern __shared__ unsigned char smem_dyn[];
     __shared__ ChunkBars bars;
     unsigned char* Qs = (unsigned char*)(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
     unsigned char* slots = Qs + C::Q_BYTES;
+    unsigned char* raws = slots + C::SLOTS * C::TILE_BYTES;
     u64* prefix = reinterpret_cast<u64*>(Qs);                    // (until the run's first unit is found)
     static_assert((CSD_MAX_SEQS + 1) * 8 <= C::Q_BYTES, "the prefix fits");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, group = a.group;
@@ -131,8 +144,9 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
     const u64 begin = run_begin(blockIdx.x, units, n_runs), end = run_begin(blockIdx.x + 1, units, n_runs);
 
     if (tid == 0) {
-        for (int i = 0; i < 8; ++i) { mbar_init(&bars.full[i], 4); mbar_init(&bars.free_[i], 1); }
-        mbar_init(&bars.qfull, 4); mbar_init(&bars.qfree, 1);
+        for (int i = 0; i < 8; ++i) { mbar_init(&bars.full[i], 4); mbar_init(&bars.free_[i], 1); mbar_init(&bars.landed[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&bars.rawfull[i], 1); mbar_init(&bars.rawfree[i], 4); }
+        mbar_init(&bars.qfull, 2); mbar_init(&bars.qfree, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars.sfull[i], 1); mbar_init(&bars.pready[i], 4); mbar_init(&bars.ofull[i], 1); mbar_init(&bars.ofree[i], 4);
             mbar_init(&bars.joined[i], 4); mbar_init(&bars.told[i], 1);
@@ -140,7 +154,7 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) {
+    if (warp == 1) {
         // behind the dependency wait: a kernel before this one may hold tensor memory until it ends
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -167,97 +181,183 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
         if (unit < end) { at.tile = p.stop - 1; at.next(w, group, false); }
     };
 
-    if (warp < 4) {
-        // ---- loaders.  Tiles in the order K, V of a position tile; each is announced two tiles later, when its copies have landed
+    if (warp < 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CH_FEWER));
+    if (warp == 0) {
+        // ---- requests, tiles in the order K, V of a position tile
         unsigned n = 0;                                          // tiles so far
+        bool ok = true;
+        // this lane's page of position tile t: lanes 0-7 have its eight groups of 16
+        auto page_of = [&](int t) {
+            const int pos = t * CH_KEYS + 16 * lane;
+            return lane < 8 && pos < at.seen ? paged_page(w, at.s, pos) : -1;
+        };
+        const int P = 1 << w.page_shift, pages = CH_KEYS >> w.page_shift;
+        while (unit < end && ok) {
+            const ChunkPiece p(w, at, end, group);
+            int page = page_of(p.first);
+            for (int t = p.first; t < p.stop && ok; ++t) {
+                const int next = t + 1 < p.stop ? page_of(t + 1) : -1;
+                const unsigned lost = __ballot_sync(0xffffffffu, lane < 8 && t * CH_KEYS + 16 * lane < at.seen && page < 0);
+                if (lane == 0) bars.lost[n >> 1 & 7] = lost;
+                const bool edge = (t + 1) * CH_KEYS > p.see[0];  // (warps 4-7 look through its values)
+#pragma unroll 1
+                for (int kv = 0; kv < 2; ++kv, ++n) {
+                    const int boxes = E4M3 ? pages : pages * C::HALVES, j = E4M3 ? lane : lane / C::HALVES;
+                    const int pg = __shfl_sync(0xffffffffu, page, min(j, pages - 1) << (w.page_shift - 4));
+                    const bool there = lane < boxes && pg >= 0;
+                    const size_t row = there ? paged_row(w, pg, at.h, 0) : 0;
+                    const int count = __popc(__ballot_sync(0xffffffffu, there));
+                    if constexpr (!E4M3) {
+                        const int slot = (int)(n % C::SLOTS);
+                        ok = n < (unsigned)C::SLOTS || warp_waits(&bars.free_[slot], (n / C::SLOTS - 1) & 1u);
+                        if (!ok) break;
+                        const bool direct = kv == 0 || !edge;
+                        uint64_t* bar = direct ? &bars.full[slot] : &bars.landed[slot];
+                        if (kv == 1 && lost) {                   // values of positions without a page: zeros
+                            for (int i = lane; i < CH_KEYS * DH / 8; i += 32) {
+                                const int key = i / (DH / 8), c = i % (DH / 8);
+                                if (lost >> (key >> 4) & 1)
+                                    *reinterpret_cast<uint4*>(slots + slot * C::TILE_BYTES + tile_off(key, c, CH_KEYS)) = make_uint4(0u, 0u, 0u, 0u);
+                            }
+                            fence_async_smem();
+                            __syncwarp();
+                        }
+                        if (lane == 0) mbar_expect_tx(bar, (uint32_t)count * (uint32_t)P * 128u);
+                        __syncwarp();
+                        if (direct && lane >= 1 && lane < 4) mbar_arrive(bar);
+                        if (there)
+                            tma_load_2d(slots + slot * C::TILE_BYTES + lane % C::HALVES * (CH_KEYS * 128) + j * P * 128, kv ? &tmV : &tmK, bar, lane % C::HALVES * 64, (int)row);
+                    } else {
+                        const int stage = (int)(n & 1u);
+                        ok = n < 2u || warp_waits(&bars.rawfree[stage], ((n >> 1) - 1) & 1u);
+                        if (!ok) break;
+                        if (lane == 0) mbar_expect_tx(&bars.rawfull[stage], (uint32_t)count * (uint32_t)(P * (DH + 1)));
+                        __syncwarp();
+                        if (there) {
+                            const uint32_t dst = smem_u32(raws) + stage * C::RAW;
+                            bulk_load(dst + j * P * DH, (kv ? w.v : w.k) + row * DH, (uint32_t)(P * DH), &bars.rawfull[stage]);
+                            bulk_load(dst + CH_KEYS * DH + j * P, (kv ? w.v_exp : w.k_exp) + row, (uint32_t)P, &bars.rawfull[stage]);
+                        }
+                    }
+                }
+                page = next;
+            }
+            advance(p);
+        }
+    } else if (warp == 2 || warp == 3) {
+        // ---- queries: the block's rows as two operand tiles of 128
         int pieces = 0;
-        uint64_t* waiting[2] = {nullptr, nullptr};               // barriers of the groups in flight, oldest first
-        auto announce = [&](uint64_t* bar) {
-            if (!bar) return;
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar);
-        };
-        auto in_flight = [&](uint64_t* bar) {
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            asm volatile("cp.async.wait_group 2;" ::: "memory");
-            announce(waiting[0]);
-            waiting[0] = waiting[1]; waiting[1] = bar; 
-        };
         bool ok = true;
         while (unit < end && ok) {
             const ChunkPiece p(w, at, end, group);
-            if (pieces > 0) {                                    // (the item before needs all its tiles to leave its queries)
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-                announce(waiting[0]);
-                announce(waiting[1]);
-                waiting[0] = waiting[1] = nullptr;
-            }
             if (pieces > 0) ok = warp_waits(&bars.qfree, (uint32_t)(pieces - 1) & 1u);
             if (!ok) break;
-            for (int i = tid; i < CH_ROWS * (DH / 8); i += 128) {
+            ++pieces;
+            for (int i = tid - 64; i < CH_ROWS * (DH / 8); i += 64) {
                 const int r = i / (DH / 8), c = i % (DH / 8), pr = p.p0 + r;
                 const bool there = r < p.nrows;
                 const size_t src = there ? (size_t)(at.q.start + pr / group) * a.ldq + (size_t)(at.h * group + pr % group) * DH + 8 * c : 0;
                 cp_async16(smem_u32(Qs) + (r >> 7) * (128 * DH * 2) + tile_off(r & 127, c, 128), (const uint16_t*)a.q + src, there);
             }
-            in_flight(&bars.qfull);
-            ++pieces;
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.qfull);
+            advance(p);
+        }
+    } else if (warp >= 4 && warp < 8) {
+        // ---- finishing tiles
+        unsigned n = 0;
+        uint32_t landings = 0;                                   // parities of landed[]
+        bool ok = true;
+        const int f = warp - 4, t128 = tid - 128;
+        while (unit < end && ok) {
+            const ChunkPiece p(w, at, end, group);
             for (int t = p.first; t < p.stop && ok; ++t) {
-                const int t0 = t * CH_KEYS, left = at.seen - t0;
-                // pages of the tile's eight groups of 16
-                int page = -1;
-                if (lane < 8 && 16 * lane < left) page = paged_page(w, at.s, t0 + 16 * lane);
-                const unsigned lost = __ballot_sync(0xffffffffu, lane < 8 && 16 * lane < left && page < 0);
-                if (tid == 0) bars.lost[n >> 1 & 7] = lost;
-#pragma unroll 1
-                for (int kv = 0; kv < 2 && ok; ++kv, ++n) {
-                    const int slot = (int)(n % C::SLOTS);
-                    if (n >= (unsigned)C::SLOTS) ok = warp_waits(&bars.free_[slot], (n / C::SLOTS - 1) & 1u);
+                const int t0 = t * CH_KEYS, left = at.seen - t0, see = p.see[0] - t0;
+                if constexpr (!E4M3) {
+                    const unsigned v = n + 1, slot = v % C::SLOTS;
+                    n += 2;
+                    if (see >= CH_KEYS) continue;
+                    ok = warp_waits(&bars.landed[slot], landings >> slot & 1u);
                     if (!ok) break;
-                    const uint32_t dst = smem_u32(slots) + slot * C::TILE_BYTES;
-                    const unsigned char* pool = kv ? w.v : w.k;
-                    if constexpr (!E4M3) {
-                        constexpr int PER = DH / 8;              // 16-byte chunks of a row
+                    landings ^= 1u << slot;
+                    // a lane a position
+                    const int key = 32 * f + lane;
+                    const bool gone = key >= left;
+                    const uint32_t rowa = smem_u32(slots) + slot * C::TILE_BYTES + key * 128;
+                    bool odd = false;
+                    if (gone || key >= see) {
+#pragma unroll 4
+                        for (int i = 0; i < DH / 8; ++i) {       // (a lane's own order, so that the banks differ)
+                            const uint32_t addr = rowa + (i >> 3) * (CH_KEYS * 128) + (((i ^ lane) & 7) << 4);
+                            uint32_t x[4] = {0u, 0u, 0u, 0u};
+                            bool change = gone;
+                            if (!gone) {
+                                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr));
 #pragma unroll
-                        for (int i = 0; i < CH_KEYS * PER / 128; ++i) {
-                            const int key = (i * 128 + tid) / PER, c = tid % PER;
-                            const int pg = __shfl_sync(0xffffffffu, page, key >> 4);
-                            const bool there = pg >= 0 && key < left;
-                            const size_t row = there ? paged_row(w, pg, at.h, t0 + key) : 0;
-                            cp_async16(dst + tile_off(key, c, CH_KEYS), pool + (row * DH + 8 * c) * 2, there);
-                        }
-                    } else {
-                        constexpr int PER = DH / 16, N = CH_KEYS * PER / 128;
-                        uint4 raw[N];
-                        unsigned e[N];
-#pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            const int key = (i * 128 + tid) / PER, c = tid % PER;
-                            const int pg = __shfl_sync(0xffffffffu, page, key >> 4);
-                            const bool there = pg >= 0 && key < left;
-                            const size_t row = there ? paged_row(w, pg, at.h, t0 + key) : 0;
-                            raw[i] = there ? *reinterpret_cast<const uint4*>(pool + row * DH + 16 * c) : make_uint4(0u, 0u, 0u, 0u);
-                            e[i] = there ? (kv ? w.v_exp : w.k_exp)[row] : 127u;
-                        }
-#pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            const int key = (i * 128 + tid) / PER, c = tid % PER;
-                            const uint32_t one = pack_bf16(row_scale(e[i]), row_scale(e[i]));
-                            const uint2 x = widen4(raw[i].x, one), y = widen4(raw[i].y, one), z = widen4(raw[i].z, one), u = widen4(raw[i].w, one);
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + tile_off(key, 2 * c, CH_KEYS)), "r"(x.x), "r"(x.y), "r"(y.x), "r"(y.y) : "memory");
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + tile_off(key, 2 * c + 1, CH_KEYS)), "r"(z.x), "r"(z.y), "r"(u.x), "r"(u.y) : "memory");
+                                for (int e = 0; e < 4; ++e)
+                                    if (odd_bf16(x[e])) {
+                                        change = odd = true;
+                                        if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
+                                        if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu;
+                                    }
+                            }
+                            if (change) asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
                         }
                     }
-                    in_flight(&bars.full[slot]);
+                    const unsigned word = __ballot_sync(0xffffffffu, odd);
+                    if (lane == 0) bars.odd[v >> 1 & 7][f] = word;
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.full[slot]);
+                } else {
+#pragma unroll 1
+                    for (int kv = 0; kv < 2; ++kv, ++n) {
+                        const int stage = (int)(n & 1u), slot = (int)(n % C::SLOTS);
+                        ok = warp_waits(&bars.rawfull[stage], (n >> 1) & 1u);
+                        if (ok) ok = n < (unsigned)C::SLOTS || warp_waits(&bars.free_[slot], (n / C::SLOTS - 1) & 1u);
+                        if (!ok) break;
+                        const unsigned lost = bars.lost[n >> 1 & 7];
+                        const unsigned char* raw = raws + stage * C::RAW;
+                        const uint32_t dst = smem_u32(slots) + slot * C::TILE_BYTES;
+                        constexpr int PER = DH / 16, STEP = 128 / PER;   // 16-byte pieces of a row, rows a turn
+                        unsigned odd = 0;
+#pragma unroll 4
+                        for (int i = 0; i < CH_KEYS / STEP; ++i) {
+                            const int key = i * STEP + t128 / PER, c = t128 % PER;
+                            const bool there = key < left && !(lost >> (key >> 4) & 1);
+                            uint4 u = *reinterpret_cast<const uint4*>(raw + key * DH + 16 * c);
+                            const unsigned e = raw[CH_KEYS * DH + key];
+                            // the scale 2^(e - 127) times 2^120, as one power where that is one
+                            unsigned field = min(e + 120u, 254u), more = e + 120u > 254u ? e + 120u - 254u + 127u : 127u;
+                            if (!there) u = make_uint4(0u, 0u, 0u, 0u), field = more = 127u;
+                            else if (e == 255u) {                // NaN; values that not every row sees are put in at the end
+                                field = 255u; more = 127u;
+                                if (kv && key >= see) { field = 0u; odd |= 1u << (key & 31); }
+                                u = field ? make_uint4(0u, 0u, 0u, 0u) : u;          // (0 x infinity)
+                            }
+                            const bool twice = __any_sync(0xffffffffu, more != 127u);
+                            const uint32_t up = two_powers(field), rest = two_powers(more);
+                            const uint2 x = widen4(u.x, up, rest, twice), y = widen4(u.y, up, rest, twice), z = widen4(u.z, up, rest, twice), v = widen4(u.w, up, rest, twice);
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + tile_off(key, 2 * c, CH_KEYS)), "r"(x.x), "r"(x.y), "r"(y.x), "r"(y.y) : "memory");
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + tile_off(key, 2 * c + 1, CH_KEYS)), "r"(z.x), "r"(z.y), "r"(v.x), "r"(v.y) : "memory");
+                        }
+                        if (kv) {
+                            odd = __reduce_or_sync(0xffffffffu, odd);    // (of positions anywhere in the tile: that some are is all that is asked)
+                            if (lane == 0) bars.odd[n >> 1 & 7][f] = odd;
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) { mbar_arrive(&bars.rawfree[stage]); mbar_arrive(&bars.full[slot]); }
+                    }
                 }
             }
             advance(p);
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        announce(waiting[0]);
-        announce(waiting[1]);
-    } else if (warp == 12) {
+    } else if (warp == 1) {
         // ---- products
         if (lane == 0) {
             constexpr uint32_t F = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);      // bf16 x bf16 -> fp32, 128 rows
@@ -316,9 +416,11 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
                 advance(p);
             }
         }
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(CH_MORE));
         // ---- softmax: a half of the block's rows, a thread a row
-        const int half = (warp - 4) >> 2, quad = warp & 3, r = 128 * half + 32 * quad + lane;
+        const int half = (warp - 8) >> 2, quad = warp & 3, r = 128 * half + 32 * quad + lane;
         const uint32_t lanes = (uint32_t)(32 * quad) << 16, S = tmem + lanes + 128 * half, O = tmem + lanes + C::O_COL + 128 * half;
         const float to_log2 = a.scale * 1.4426950408889634f;
         uint32_t tiles_done = 0, run_tiles = 0, joins = 0;
@@ -330,6 +432,7 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
             const bool mine = r < p.nrows;
             const int lim = mine ? min(at.q.kv + token + 1, w.capacity) : 0;
             float m = -INFINITY, l = 0.f;
+            bool odd = false;                                    // values were taken out of the run's tiles
             for (int t = p.first; t < p.end[half] && ok; ++t) {
                 ok = warp_waits(&bars.sfull[half], tiles_done & 1u);
                 if (!ok) break;
@@ -348,16 +451,18 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
                 tm_ld32(S + 96, y);
                 tm_wait_ld();
                 if (edge) { mask(x, 64); mask(y, 96); }
-                float top = fmaxf(x[0], y[0]);
+                float tops[4];
 #pragma unroll
-                for (int j = 1; j < 32; ++j) top = fmaxf(top, fmaxf(x[j], y[j]));
+                for (int j = 0; j < 4; ++j) tops[j] = fmaxf(x[j], y[j]);
+#pragma unroll
+                for (int j = 4; j < 32; ++j) tops[j & 3] = fmaxf(tops[j & 3], fmaxf(x[j], y[j]));
                 tm_ld32(S, x);
                 tm_ld32(S + 32, y);
                 tm_wait_ld();
                 if (edge) { mask(x, 0); mask(y, 32); }
 #pragma unroll
-                for (int j = 0; j < 32; ++j) top = fmaxf(top, fmaxf(x[j], y[j]));
-                top *= to_log2;                                  // (the scale is positive here)
+                for (int j = 0; j < 32; ++j) tops[j & 3] = fmaxf(tops[j & 3], fmaxf(x[j], y[j]));
+                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * to_log2;                                  // (the scale is positive here)
                 if (__any_sync(0xffffffffu, top > m + CH_LATE)) {
                     const float nm = fmaxf(m, top), keep = nm == -INFINITY ? 0.f : ex2(m - nm);
                     m = nm;
@@ -375,13 +480,13 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
                     }
                 }
                 const float base = m == -INFINITY ? 0.f : m;
-                float sum = 0.f, sum2 = 0.f;
+                float sums[4] = {0.f, 0.f, 0.f, 0.f};
                 auto weights = [&](float (&s)[32], int col) {
                     uint32_t u[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         const float e0 = ex2(fmaf(s[2 * j], to_log2, -base)), e1 = ex2(fmaf(s[2 * j + 1], to_log2, -base));
-                        sum += e0; sum2 += e1;
+                        sums[2 * (j & 1)] += e0; sums[2 * (j & 1) + 1] += e1;
                         u[j] = pack_bf16(e0, e1);
                     }
                     tm_st16(S + col, u);
@@ -394,7 +499,7 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
                 if (edge) { mask(x, 64); mask(y, 96); }
                 weights(x, 32);
                 weights(y, 48);
-                l += sum + sum2;
+                l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
                 tm_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -404,14 +509,25 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
             // ---- the rows leave, finished or as a part of their item
             const bool any = p.first < p.end[half];
             if (any) {
+                // (the products of these tiles have read their values, so what was noted of them stands)
                 ok = warp_waits(&bars.ofull[half], (uint32_t)rounds & 1u);
                 if (!ok) break;
                 ++rounds;
                 tc_fence_after();
+                for (int t = max(p.first, p.end[half] - 4); t < p.end[half]; ++t) {
+                    const unsigned i = (run_tiles + (unsigned)(t - p.first)) & 7;
+                    if ((t + 1) * CH_KEYS > p.see[0]) odd |= (bars.odd[i][0] | bars.odd[i][1] | bars.odd[i][2] | bars.odd[i][3]) != 0;
+                }
             }
             float* part = a.parts + ((size_t)blockIdx.x * 2 + (p.first == 0 ? 1 : 0)) * C::PART;
             const size_t dst = mine ? (size_t)(at.q.start + token) * a.ldo + (size_t)(at.h * group + p_row % group) * DH : 0;
             const float inv = l == 0.f ? 0.f : 1.f / l;
+            auto store_row = [&](size_t to, const float (&o)[32], float f) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 8)
+                    *reinterpret_cast<uint4*>((uint16_t*)a.out + to + j) = make_uint4(pack_bf16(o[j] * f, o[j + 1] * f), pack_bf16(o[j + 2] * f, o[j + 3] * f),
+                                                                                      pack_bf16(o[j + 4] * f, o[j + 5] * f), pack_bf16(o[j + 6] * f, o[j + 7] * f));
+            };
             if (any) {
 #pragma unroll 1
                 for (int c = 0; c < DH; c += 32) {
@@ -419,16 +535,22 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
                     tm_ld32(O + c, o);
                     tm_wait_ld();
                     if (!mine) continue;
-                    if (p.whole) {
+                    if (odd)                                     // infinities and NaN that this row sees
+                        for (int pos = max(p.see[0], p.first * CH_KEYS); pos < min(lim, p.stop * CH_KEYS); ++pos) {
+                            const int pg = paged_page(w, at.s, pos);
+                            const size_t row = pg >= 0 ? paged_row(w, pg, at.h, pos) : 0;
+                            if (pg < 0 || (E4M3 && w.v_exp[row] != 255u)) continue;
 #pragma unroll
-                        for (int j = 0; j < 32; j += 8)
-                            *reinterpret_cast<uint4*>((uint16_t*)a.out + dst + c + j) =
-                                make_uint4(pack_bf16(o[j] * inv, o[j + 1] * inv), pack_bf16(o[j + 2] * inv, o[j + 3] * inv),
-                                           pack_bf16(o[j + 4] * inv, o[j + 5] * inv), pack_bf16(o[j + 6] * inv, o[j + 7] * inv));
+                            for (int j = 0; j < 32; ++j) {
+                                const float v = E4M3 ? __uint_as_float(0x7fffffffu) : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(w.v)[row * DH + c + j]);
+                                if (!(fabsf(v) < INFINITY)) o[j] += v;
+                            }
+                        }
+                    if (p.whole) {
+                        store_row(dst + c, o, inv);
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4)
-                            __stcg(reinterpret_cast<float4*>(part + (size_t)r * DH + c + j), make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+                        for (int j = 0; j < 32; ++j) __stcg(part + (half * DH + c + j) * 128 + 32 * quad + lane, o[j]);
                     }
                 }
                 tc_fence_before();
@@ -463,24 +585,22 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
                         top = base;
                     }
                     const float scale = total == 0.f ? 0.f : 1.f / total;
-                    // a warp its 32 rows, lanes along a row
-                    constexpr int PER = DH / 4;
-                    for (int i = lane; i < 32 * PER; i += 32) {
-                        const int rr = i / PER, row = 128 * half + 32 * quad + rr, d = i % PER * 4;
-                        const float row_top = __shfl_sync(0xffffffffu, top, rr), row_scale_ = __shfl_sync(0xffffffffu, scale, rr);
-                        if (row >= p.nrows) continue;
-                        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                        for (int c = c0; c <= c1; ++c) {
-                            const float pm = __ldcg(of(c) + CH_ROWS * DH + row);
-                            if (pm == -INFINITY) continue;       // (nothing was written of the rows)
-                            const float f = ex2(pm - row_top);
-                            const float4 x = __ldcg(reinterpret_cast<const float4*>(of(c) + (size_t)row * DH + d));
-                            v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
+                    if (mine) {
+#pragma unroll 1
+                        for (int c = 0; c < DH; c += 32) {
+                            float o[32];
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) o[j] = 0.f;
+                            for (int k = c0; k <= c1; ++k) {
+                                const float pm = __ldcg(of(k) + CH_ROWS * DH + r);
+                                if (pm == -INFINITY) continue;   // (nothing was written of the row)
+                                const float f = ex2(pm - top);
+                                const float* src = of(k) + (half * DH + c) * 128 + 32 * quad + lane;
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) o[j] = fmaf(f, __ldcg(src + j * 128), o[j]);
+                            }
+                            store_row(dst + c, o, scale);
                         }
-                        const int pp = p.p0 + row;
-                        const size_t to = (size_t)(at.q.start + pp / group) * a.ldo + (size_t)(at.h * group + pp % group) * DH + d;
-                        *reinterpret_cast<uint2*>((uint16_t*)a.out + to) =
-                            make_uint2(pack_bf16(v.x * row_scale_, v.y * row_scale_), pack_bf16(v.z * row_scale_, v.w * row_scale_));
                     }
                 }
             }
@@ -494,25 +614,31 @@ paged_chunk_kernel(const PagedView w, const AttendArgs a, int least_units) {
         if (tid == 0) set_status(w.status, CSD_ERR_TIMEOUT);
         __nanosleep(2000000);                    // let products already issued end before the CTA's memory is released
     }
-    if (warp == 12) {
+    if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
 }
 
 template <int DH, bool E4M3> static csd_status run_chunk(const PagedView& w, const AttendArgs& a, cudaStream_t st) {
+    using C = ChunkCfg<DH, E4M3>;
     auto kern = paged_chunk_kernel<DH, E4M3>;
     static PerDevice ready;
-    const csd_status ok = allow_smem(ready, kern, ChunkCfg<DH>::SMEM);
+    const csd_status ok = allow_smem(ready, kern, C::SMEM);
     if (ok != CSD_OK) return ok;
-    PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(CH_THREADS), ChunkCfg<DH>::SMEM, st);
-    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a, 1));
+    CUtensorMap tk = {}, tv = {};
+    if constexpr (!E4M3) {
+        const int rows = w.n_pages * w.heads << w.page_shift;    // (below 2^31: paged_view)
+        if (!encode_map_2d(w.k, rows, DH, 1 << w.page_shift, &tk) || !encode_map_2d(w.v, rows, DH, 1 << w.page_shift, &tv)) return CSD_ERR_UNSUPPORTED;
+    }
+    PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(CH_THREADS), C::SMEM, st);
+    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, tk, tv, w, a, 1));
     count_launch();
     return CSD_OK;
 }
 
 size_t paged_chunk_workspace(int d_head) {
-    return PAGED_TICKET_BYTES + (size_t)tc_sm_count() * 2 * (d_head == 64 ? ChunkCfg<64>::PART : ChunkCfg<128>::PART) * 4;
+    return PAGED_TICKET_BYTES + (size_t)tc_sm_count() * 2 * (d_head == 64 ? ChunkCfg<64, false>::PART : ChunkCfg<128, false>::PART) * 4;
 }
 
 csd_status launch_paged_chunk(const PagedView& w, AttendArgs a, int d_head, void* workspace, cudaStream_t st) {

@@ -40,9 +40,6 @@ template <int DH, int MT, bool ROWS16, bool E4M3> struct PagedRowsCfg {
     static constexpr int PART = BR * (DH + 2);                           // floats of a part: rows, maxima, sums
 };
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -61,10 +58,6 @@ __device__ __forceinline__ uint32_t e4m3_to_bf16(uint32_t w, bool odd) {
     uint32_t r = odd ? ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u) : ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u);
     asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(r) : "r"(0x7b807b80u));
     return r;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-    return *reinterpret_cast<const uint32_t*>(&h);
 }
 // byte offset of 16-byte chunk c of row j, so that ldmatrix reads eight rows without conflict
 template <int RB> __device__ __forceinline__ uint32_t stage_off(int j, int c) {
@@ -340,7 +333,50 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units) {
                         }
                         l[mt][hr] += sum;
                     }
-                // ---- output += weights . values
+                // ---- output += weights . values.  0 x NaN is NaN: where some rows do not see all of the positions, infinities and NaN
+                //      among their values send the warp through them one by one (fp32 rows everywhere: an infinity times a weight's
+                //      terms is one less another)
+                bool odd = false;
+                if (edge || !ROWS16) {
+                    const int key = lane >> 1;
+                    if constexpr (E4M3) {
+                        odd = t0 + key < at.seen && (stages + slot * C::STAGE + 32 * C::RB)[16 + key] == 255u;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < C::RB / 32; ++i) {
+                            const uint4 u = *reinterpret_cast<const uint4*>(stages + slot * C::STAGE + 16 * C::RB + key * C::RB + ((2 * i + (lane & 1)) << 4));
+                            odd |= odd_bf16(u.x) || odd_bf16(u.y) || odd_bf16(u.z) || odd_bf16(u.w);
+                        }
+                    }
+                }
+                if (__any_sync(0xffffffffu, odd)) {
+                    const unsigned char* vt = stages + slot * C::STAGE + 16 * C::RB;
+#pragma unroll 1
+                    for (int key = 0; key < 16; ++key) {
+                        const int from = (lane & ~3) | ((key & 7) >> 1);
+                        const float vs = E4M3 ? row_scale(vt[16 * C::RB + 16 + key]) : 1.f;
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (int hr = 0; hr < 2; ++hr) {
+                                const float a0 = key < 8 ? s[mt][0][2 * hr] : s[mt][1][2 * hr], a1 = key < 8 ? s[mt][0][2 * hr + 1] : s[mt][1][2 * hr + 1];
+                                const float x = __shfl_sync(0xffffffffu, key & 1 ? a1 : a0, from);
+                                if (x == -INFINITY) continue;            // (not seen)
+                                const float weight = exp2f(x - m[mt][hr]);
+#pragma unroll
+                                for (int t = 0; t < DH / 8; ++t)
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        float v;
+                                        if constexpr (E4M3)
+                                            v = __half2float(__ushort_as_half((unsigned short)e4m3_to_f16(vt[stage_off<C::RB>(key, t >> 1) + 4 * (lane & 3) + 2 * e + (t & 1)]))) * vs;
+                                        else
+                                            v = bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(vt + stage_off<C::RB>(key, t) + 2 * (2 * (lane & 3) + e)));
+                                        o[mt][t][2 * hr + e] = fmaf(weight, v, o[mt][t][2 * hr + e]);
+                                    }
+                            }
+                    }
+                } else
 #pragma unroll
                 for (int j = 0; j < C::RB / 32; ++j) {
                     uint32_t vb[4];

@@ -12,7 +12,8 @@ constexpr int STAGE_BYTES = TILE_N * KB * 2;      // 16 KB
 constexpr int SPIN_LIMIT = 20000000;              // bounded waits (about a second)
 
 // [rows][K] bf16 row-major, boxes of box_rows x 64 elements, 128-byte swizzle, zero fill outside
-bool tensor_map_2d(const void* base, int rows, int K, int box_rows, CUtensorMap* out);
+bool encode_map_2d(const void* base, int rows, int K, int box_rows, CUtensorMap* out);
+bool tensor_map_2d(const void* base, int rows, int K, int box_rows, CUtensorMap* out);      // kept from call to call
 int tc_sm_count();
 
 // ---- device-side PTX helpers -------------------------------------------------------------------

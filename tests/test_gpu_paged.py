@@ -145,6 +145,42 @@ def test_rows_that_see_nothing(b, dtype):
     assert (out[[0, 3, 5, 10, 44]] == 0).all()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,kv,heads,kv_heads,dim,tree", [((6, 5), (40, 0), 4, 2, 128, False), ((7,), (9,), 2, 2, 64, True), ((300, 40), (30, 500), 4, 2, 128, False),
+                                                             ((150,), (0,), 4, 1, 64, False)])
+def test_odd_numbers_stay_with_the_rows_that_see_them(b, kind, dtype, rows, kv, heads, kv_heads, dim, tree):
+    """Infinities and NaN in keys and values of new rows: rows that do not see them are what they are without them."""
+    c = pp.Case(b, rows, kv, kv_heads, dim, 16, kind, dtype, seed=7)
+    masks = pp.trees(rows, 11) if tree else None
+    g = torch.Generator().manual_seed(3)
+    q = [torch.randn(r, heads, dim, generator=g) for r in rows]
+    first = [3 * r // 5 for r in rows]                     # rows before this one see none of them
+    for s, (r, n) in enumerate(zip(rows, kv)):
+        at = n + first[s]
+        c.vals[s][at, 0, 5], c.vals[s][at, 0, 6] = float("nan"), float("inf")
+        if kind == "bf16":
+            c.vals[s][at + 1, -1, 9], c.vals[s][n + r - 1, 0, dim - 1] = -float("inf"), float("inf")
+        c.keys[s][n + r - 1, -1, 0] = float("nan")
+    c.fill()
+    out = torch.full((c.total, heads, dim), -7.0, dtype=dtype, device="cuda")
+    tm = torch.tensor(masks + [0] * (c.total - len(masks)), dtype=torch.int64).cuda() if tree else None
+    b.csd_paged_attention(c.packed(q), c.pool, c.batch(), tree_mask=tm, out=out)
+    got = out.double().cpu().numpy()
+    for s, (r, n) in enumerate(zip(rows, kv)):
+        mine = None if masks is None else masks[c.start[s]:c.start[s + 1]]
+        with np.errstate(invalid="ignore"):
+            want, size, top = pp.attention(q[s].to(dtype).double().numpy(), c.held(c.keys[s]), c.held(c.vals[s]), n, dim ** -0.5, mine)
+        far = got[c.start[s]:c.start[s + 1]]
+        fine = np.isfinite(want)
+        assert np.array_equal(fine, np.isfinite(far)) and np.array_equal(np.isnan(want), np.isnan(far))
+        assert np.array_equal(want[~fine & ~np.isnan(want)], far[~fine & ~np.isnan(want)])
+        assert fine[:first[s]].all() or tree
+        top = 40.0                                        # (scores of finite keys here are far below; the plain form's bound is NaN)
+        bound = pp.attention_bound(np.where(fine, want, 0), np.where(fine, size, 0), top, n + r, dim, dtype)
+        assert (np.abs(np.where(fine, far, 0) - np.where(fine, want, 0)) <= bound).all()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("scale,amplitude", [(0.0, 1.0), (-0.2, 1.0), (3.0, 1.0), (1.0, 12.0)])
 def test_scales(b, dtype, scale, amplitude):
