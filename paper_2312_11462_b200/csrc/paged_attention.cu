@@ -8,13 +8,13 @@ static csd_status check_attend(const csd_kv_pool* pool, const csd_paged_batch* b
     const csd_status ok = paged_view(pool, batch, w);
     if (ok != CSD_OK) return ok;
     if (n_heads < 1 || n_heads % pool->n_kv_heads || n_heads / pool->n_kv_heads > 64) return CSD_ERR_SHAPE;
-    return row_type == CSD_F32 || row_type == CSD_BF16 ? CSD_OK : CSD_ERR_INVALID_ARG;
+    if (row_type != CSD_F32 && row_type != CSD_BF16) return CSD_ERR_INVALID_ARG;
+    return (long long)batch->max_rows * (n_heads / pool->n_kv_heads) < 1 << 30 ? CSD_OK : CSD_ERR_CAPACITY;
 }
 
 // (row, query head) pairs of one sequence and kv head at most
 static int packed_rows(const csd_paged_batch* batch, const csd_kv_pool* pool, int n_heads) {
-    const long long n = (long long)batch->max_rows * (n_heads / pool->n_kv_heads);
-    return n > 1 << 30 ? 1 << 30 : (int)n;
+    return batch->max_rows * (n_heads / pool->n_kv_heads);
 }
 
 static bool takes_chunks(int packed, int row_type) { return row_type == CSD_BF16 && packed > 32; }

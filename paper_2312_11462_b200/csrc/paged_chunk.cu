@@ -6,12 +6,12 @@
 //      each); warp 1 issues tcgen05.mma, scores S = Q K^T from shared memory and output O += P V with P from tensor memory; warps 2 and 3
 //      gather the block's queries
 //   1  widens 8-bit tiles to bf16 (value times scale is exact there), and puts bf16 tiles of values that not every row sees in order
-//   2, 3  a half of the rows each, a thread a row: running maximum, exponentials, P as bf16 over the scores' columns.  The halves alternate,
-//      so that one's products run under the other's exponentials.  They take most of the registers.
-// The output stays in tensor memory; it is rescaled only when a maximum has grown by more than 2^8.
-//
-// All products of a CTA are issued by one thread and run in order: when S of tile t + 1 is there, O += P V of tile t is done, so a
-// softmax thread may rescale O without another barrier, and S may overwrite the P that the product before it has read.
+//   2, 3  a half of the rows each, a thread a row: running maximum, exponentials, P as bf16 over the scores' columns.  They take most of
+//      the registers.
+// Tensor memory (512 columns): per half the scores of a tile, 128 columns that P overwrites, and the output.  All products of a CTA are
+// issued by one thread and run in order, so when the scores of tile t + 1 are there, O += P V of tile t is done.  P goes out in two parts of 64
+// positions; the first one's product runs under the other's exponentials.  A running maximum is only brought up when a score is above it by 2^16
+// (bf16 and fp32 have room for that), so that hardly a tile after an item's first waits for its maximum or rescales the output.
 //
 // What lies behind a sequence's positions may be anything, and 0 x NaN is NaN: values behind the last position are zeroed, and so
 // are infinities and NaN in positions that some of the block's rows do not see; rows that see them get them added at the end.
@@ -21,9 +21,9 @@
 namespace csd {
 
 constexpr int CH_KEYS = 128, CH_ROWS = 256, CH_THREADS = 512;
-constexpr int CH_MORE = 168, CH_FEWER = 88;     // registers of a softmax thread and of the others: 512 threads are launched with 128 each
+constexpr int CH_MORE = 136, CH_FEWER = 120;     // registers of a softmax thread and of the others: 512 threads are launched with 128 each
 static_assert(256 * CH_MORE + 256 * CH_FEWER <= 512 * 128, "a setmaxnreg.inc beyond the launch's registers would wait for good");
-constexpr float CH_LATE = 8.f;                  // a running maximum may lag by this power of two
+constexpr float CH_LATE = 16.f;                 // a running maximum may lag by this power of two (bf16 and fp32 have room for it)
 
 template <int DH, bool E4M3> struct ChunkCfg {
     static constexpr int HALVES = DH / 64;                       // 64-column halves of a row, 128 bytes each
@@ -38,7 +38,7 @@ template <int DH, bool E4M3> struct ChunkCfg {
 };
 
 struct ChunkBars {
-    uint64_t full[8], free_[8], landed[8], rawfull[2], rawfree[2], qfull, qfree, sfull[2], pready[2], ofull[2], ofree[2], joined[2], told[2];
+    uint64_t full[8], free_[8], landed[8], rawfull[2], rawfree[2], qfull, qfree, sfull[2], pready[2][2], firsthalf[2], ofull[2], ofree[2], joined[2], told[2];
     uint32_t tmem;
     int abort_flag, last[2];
     // of the run's last eight position tiles: groups of 16 without a page; positions with values that were taken out
@@ -64,20 +64,27 @@ __device__ __forceinline__ void tm_ld32(uint32_t addr, float (&v)[32]) {
                    "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
                  : "r"(addr));
 }
-__device__ __forceinline__ void tm_st32(uint32_t addr, const float (&v)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
-                 ::"f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]),
-                   "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]),
-                   "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31]), "r"(addr) : "memory");
-}
 __device__ __forceinline__ void tm_st16(uint32_t addr, const uint32_t (&v)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
                  ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
                    "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(addr) : "memory");
 }
+__device__ __forceinline__ void tm_st16(uint32_t addr, const float (&v)[16]) {
+    uint32_t u[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) u[j] = __float_as_uint(v[j]);
+    tm_st16(addr, u);
+}
 __device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+// pairs of fp32 numbers in one register pair
+__device__ __forceinline__ u64 two(float x, float y) { u64 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y)); return r; }
+__device__ __forceinline__ float low(u64 x) { return __uint_as_float((unsigned)x); }
+__device__ __forceinline__ float high(u64 x) { return __uint_as_float((unsigned)(x >> 32)); }
+__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) { u64 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ u64 add2(u64 a, u64 b) { u64 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 // four e4m3 numbers times a power of two, `up` times `rest` less the 2^120 that the exponent fields lie apart, as two words of two bf16
 __device__ __forceinline__ uint2 widen4(uint32_t w, uint32_t up, uint32_t rest, bool twice) {
     w = __byte_perm(w, 0, 0x3120);                               // numbers 0, 2, 1, 3
@@ -100,11 +107,29 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 // byte offset of 16-byte chunk c of row r in a tile of `rows` rows: 64-column halves one behind the other, 128-byte swizzle
 __device__ __forceinline__ uint32_t tile_off(int r, int c, int rows) { return (uint32_t)((c >> 3) * (rows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 
+__device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded; gives up for the CTA, or because another of its warps has.  (Kept out of the way of waits that are over at once: with the flag
+// read in front of each, the products' thread spent 0.18 us on every one of the six of a tile.)
+__device__ __forceinline__ bool wait_long(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
+    for (int i = 0; i < SPIN_LIMIT; ++i) {
+        if (mbar_try(bar, parity)) return true;
+        if ((i & 63) == 63 && *gave_up) return false;
+    }
+    *gave_up = 1;
+    return false;
+}
+
 typedef Schedule<CH_ROWS, CH_KEYS> ChunkSchedule;
 
 // What a run has of an item, and the halves' own ends.
 struct ChunkPiece {
-    int first, stop, p0, nrows, end[2], see[2];                  // see: positions that all rows of the half see
+    int first, stop, p0, nrows;
+    int end[2], see[2];                                          // a half's last tile + 1, positions that all its rows see
     bool whole;
     __device__ __forceinline__ ChunkPiece(const PagedView& w, const ChunkSchedule::Cursor& at, u64 run_end, int group) {
         const u64 item_end = at.item_first + at.tiles;
@@ -125,7 +150,7 @@ struct ChunkPiece {
 
 template <int DH, bool E4M3>
 __global__ void __launch_bounds__(CH_THREADS, 1)
-paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PagedView w, const AttendArgs a, int least_units) {
+paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PagedView w, const AttendArgs a, int least_units, int snap) {
     using C = ChunkCfg<DH, E4M3>;
     extern __shared__ unsigned char smem_dyn[];
     __shared__ ChunkBars bars;
@@ -141,14 +166,17 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     const u64 units = prefix[w.n_seqs], most = units / (unsigned)least_units;
     const unsigned n_runs = most < 1 ? 1u : most < gridDim.x ? (unsigned)most : gridDim.x;
     if (blockIdx.x >= n_runs || units == 0) return;
-    const u64 begin = run_begin(blockIdx.x, units, n_runs), end = run_begin(blockIdx.x + 1, units, n_runs);
+    u64 begin, end;
+    ChunkSchedule::Cursor at;
+    if (!ChunkSchedule::run(w, prefix, blockIdx.x, n_runs, snap, group, false, &begin, &end, &at)) return;
 
     if (tid == 0) {
         for (int i = 0; i < 8; ++i) { mbar_init(&bars.full[i], 4); mbar_init(&bars.free_[i], 1); mbar_init(&bars.landed[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&bars.rawfull[i], 1); mbar_init(&bars.rawfree[i], 4); }
         mbar_init(&bars.qfull, 2); mbar_init(&bars.qfree, 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&bars.sfull[i], 1); mbar_init(&bars.pready[i], 4); mbar_init(&bars.ofull[i], 1); mbar_init(&bars.ofree[i], 4);
+            mbar_init(&bars.sfull[i], 1); mbar_init(&bars.pready[i][0], 4); mbar_init(&bars.pready[i][1], 4);
+            mbar_init(&bars.firsthalf[i], 1); mbar_init(&bars.ofull[i], 1); mbar_init(&bars.ofree[i], 4);
             mbar_init(&bars.joined[i], 4); mbar_init(&bars.told[i], 1);
         }
         bars.abort_flag = 0;
@@ -159,20 +187,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars.tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    ChunkSchedule::Cursor at;
-    at.seek(w, prefix, begin, group, false);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = bars.tmem;
     volatile int* gave_up = &bars.abort_flag;
     pdl_trigger();
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (*gave_up) return false;
-        if (mbar_wait(bar, parity)) return true;
-        *gave_up = 1;
-        return false;
-    };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_try(bar, parity) || wait_long(bar, parity, gave_up); };
     auto warp_waits = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
 
     u64 unit = begin;
@@ -254,11 +275,21 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             if (pieces > 0) ok = warp_waits(&bars.qfree, (uint32_t)(pieces - 1) & 1u);
             if (!ok) break;
             ++pieces;
-            for (int i = tid - 64; i < CH_ROWS * (DH / 8); i += 64) {
-                const int r = i / (DH / 8), c = i % (DH / 8), pr = p.p0 + r;
+            // row r of the block is the (rem + r)-th (token, head) pair behind the block's first token
+            constexpr int PER = DH / 8, STEP = 64 / PER;
+            const int c = (tid - 64) % PER, r0 = (tid - 64) / PER, first = p.p0 % group + r0, token = p.p0 / group + first / group;
+            const int tokens = STEP / group, heads = STEP % group;               // of a turn
+            const int64_t turn = (int64_t)tokens * a.ldq + heads * DH, wrap = a.ldq - (int64_t)group * DH;
+            int head = first % group;
+            const uint16_t* src = (const uint16_t*)a.q + (size_t)(at.q.start + token) * a.ldq + (size_t)(at.h * group + head) * DH + 8 * c;
+            const uint32_t q0 = smem_u32(Qs);
+#pragma unroll 8
+            for (int r = r0; r < CH_ROWS; r += STEP) {
                 const bool there = r < p.nrows;
-                const size_t src = there ? (size_t)(at.q.start + pr / group) * a.ldq + (size_t)(at.h * group + pr % group) * DH + 8 * c : 0;
-                cp_async16(smem_u32(Qs) + (r >> 7) * (128 * DH * 2) + tile_off(r & 127, c, 128), (const uint16_t*)a.q + src, there);
+                cp_async16(q0 + (r >> 7) * (128 * DH * 2) + tile_off(r & 127, c, 128), there ? (const void*)src : a.q, there);
+                src += turn;
+                head += heads;
+                if (head >= group) { head -= group; src += wrap; }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
             asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -363,12 +394,13 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             constexpr uint32_t F = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);      // bf16 x bf16 -> fp32, 128 rows
             constexpr uint32_t IDESC_S = F | ((uint32_t)(CH_KEYS >> 3) << 17), IDESC_O = F | (1u << 16) | ((uint32_t)(DH >> 3) << 17);   // (V: N along the rows)
             const uint64_t qd = smem_desc_sw128(smem_u32(Qs)), kd = smem_desc_sw128(smem_u32(slots)), vd = smem_desc_sw128_mn(smem_u32(slots), CH_KEYS * 128);
-            unsigned n = 0;                                      // tile of the K of the piece's first position tile
+            uint32_t slot = 0, phase = 0;                        // of the next tile to be multiplied
             int pieces = 0, rounds[2] = {0, 0};                  // pieces that a half had tiles of
-            uint32_t tiles_done[2] = {0, 0};
+            uint32_t done[2] = {0, 0};                           // position tiles of a half
             bool ok = true;
-            auto scores = [&](int i, unsigned tile) {
-                const uint64_t q = qd + (uint64_t)((i * 128 * DH * 2) >> 4), k = kd + (uint64_t)((tile % C::SLOTS * C::TILE_BYTES) >> 4);
+            auto past = [&]() { if (++slot == (uint32_t)C::SLOTS) { slot = 0; phase ^= 1u; } };
+            auto scores = [&](int i, uint32_t of) {
+                const uint64_t q = qd + (uint64_t)((i * 128 * DH * 2) >> 4), k = kd + (uint64_t)(of * (C::TILE_BYTES >> 4));
 #pragma unroll
                 for (int ks = 0; ks < DH / 16; ++ks) {
                     const uint32_t off = (uint32_t)((ks >> 2) * (128 * 128) + (ks & 3) * 32) >> 4;
@@ -378,38 +410,48 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             };
             while (unit < end && ok) {
                 const ChunkPiece p(w, at, end, group);
-                ok = wait(&bars.qfull, (uint32_t)pieces & 1u);
-                if (ok) ok = wait(&bars.full[n % C::SLOTS], (n / C::SLOTS) & 1u);
+                ok = wait(&bars.qfull, (uint32_t)pieces & 1u) && wait(&bars.full[slot], phase);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    if (p.first < p.end[i]) scores(i, n);
-                tc_commit(&bars.free_[n % C::SLOTS]);
+                    if (p.first < p.end[i]) scores(i, slot);
+                tc_commit(&bars.free_[slot]);
+                past();
                 if (p.stop == p.first + 1) tc_commit(&bars.qfree);
-                for (int t = p.first; t < p.stop && ok; ++t, n += 2) {
-                    const unsigned v = n + 1, k = n + 2;
+                for (int t = p.first; t < p.stop && ok; ++t) {
                     const bool more = t + 1 < p.stop;
-                    ok = wait(&bars.full[v % C::SLOTS], (v / C::SLOTS) & 1u);
-                    if (ok && more) ok = wait(&bars.full[k % C::SLOTS], (k / C::SLOTS) & 1u);
+                    const uint32_t v = slot;                     // this tile's values, and behind them the next one's keys
+                    ok = wait(&bars.full[slot], phase);
+                    past();
+                    const uint32_t k = slot;
+                    if (more) {
+                        ok = ok && wait(&bars.full[slot], phase);
+                        past();
+                    }
+                    const uint64_t vt = vd + (uint64_t)(v * (C::TILE_BYTES >> 4));
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         if (!ok || t >= p.end[i]) continue;
                         if (t == p.first && rounds[i] > 0) ok = wait(&bars.ofree[i], (uint32_t)(rounds[i] - 1) & 1u);
-                        if (ok) ok = wait(&bars.pready[i], tiles_done[i] & 1u);
-                        if (!ok) continue;
-                        ++tiles_done[i];
-                        tc_fence_after();
-                        const uint64_t vt = vd + (uint64_t)((v % C::SLOTS * C::TILE_BYTES) >> 4);
 #pragma unroll
-                        for (int ks = 0; ks < CH_KEYS / 16; ++ks)
-                            tc_mma_ts(tmem + C::O_COL + 128 * i, tmem + 128 * i + 8 * ks, vt + (uint64_t)((ks * 2048) >> 4), IDESC_O, t > p.first || ks > 0);
+                        for (int j = 0; j < 2; ++j) {            // weights of positions 0-63, then the others
+                            ok = ok && wait(&bars.pready[i][j], done[i] & 1u);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll
+                            for (int ks = 4 * j; ks < 4 * j + 4; ++ks)
+                                tc_mma_ts(tmem + C::O_COL + 128 * i, tmem + 128 * i + 8 * ks, vt + (uint64_t)((ks * 2048) >> 4), IDESC_O, t > p.first || ks > 0);
+                            if (j == 0) tc_commit(&bars.firsthalf[i]);
+                        }
+                        if (!ok) continue;
+                        ++done[i];
                         if (t + 1 == p.end[i]) { tc_commit(&bars.ofull[i]); ++rounds[i]; }
                         if (t + 1 < p.end[i]) scores(i, k);
                     }
                     if (!ok) break;
-                    tc_commit(&bars.free_[v % C::SLOTS]);
-                    if (more) tc_commit(&bars.free_[k % C::SLOTS]);
+                    tc_commit(&bars.free_[v]);
+                    if (more) tc_commit(&bars.free_[k]);
                     if (t + 2 == p.stop) tc_commit(&bars.qfree);
                 }
                 ++pieces;
@@ -423,7 +465,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const int half = (warp - 8) >> 2, quad = warp & 3, r = 128 * half + 32 * quad + lane;
         const uint32_t lanes = (uint32_t)(32 * quad) << 16, S = tmem + lanes + 128 * half, O = tmem + lanes + C::O_COL + 128 * half;
         const float to_log2 = a.scale * 1.4426950408889634f;
-        uint32_t tiles_done = 0, run_tiles = 0, joins = 0;
+        const u64 by = two(to_log2, to_log2);
+        uint32_t done = 0, run_tiles = 0, joins = 0;             // position tiles of the half, of the run, items joined so far
         int rounds = 0;
         bool ok = true;
         while (unit < end && ok) {
@@ -433,77 +476,86 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             const int lim = mine ? min(at.q.kv + token + 1, w.capacity) : 0;
             float m = -INFINITY, l = 0.f;
             bool odd = false;                                    // values were taken out of the run's tiles
-            for (int t = p.first; t < p.end[half] && ok; ++t) {
-                ok = warp_waits(&bars.sfull[half], tiles_done & 1u);
+            for (int t = p.first; t < p.end[half]; ++t, ++done) {
+                ok = warp_waits(&bars.sfull[half], done & 1u);
                 if (!ok) break;
-                ++tiles_done;
                 tc_fence_after();
-                const unsigned lost = bars.lost[(run_tiles + (t - p.first)) & 7];
-                const int sees = lim - t * CH_KEYS;              // of the tile's positions
-                const bool edge = (t + 1) * CH_KEYS > p.see[half] || lost != 0;
-                auto mask = [&](float (&x)[32], int j0) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (j0 + j >= sees || (lost >> ((j0 + j) >> 4) & 1)) x[j] = -INFINITY;
-                };
                 float x[32], y[32];
-                tm_ld32(S + 64, x);
-                tm_ld32(S + 96, y);
-                tm_wait_ld();
-                if (edge) { mask(x, 64); mask(y, 96); }
-                float tops[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) tops[j] = fmaxf(x[j], y[j]);
-#pragma unroll
-                for (int j = 4; j < 32; ++j) tops[j & 3] = fmaxf(tops[j & 3], fmaxf(x[j], y[j]));
                 tm_ld32(S, x);
                 tm_ld32(S + 32, y);
-                tm_wait_ld();
-                if (edge) { mask(x, 0); mask(y, 32); }
-#pragma unroll
-                for (int j = 0; j < 32; ++j) tops[j & 3] = fmaxf(tops[j & 3], fmaxf(x[j], y[j]));
-                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * to_log2;                                  // (the scale is positive here)
-                if (__any_sync(0xffffffffu, top > m + CH_LATE)) {
-                    const float nm = fmaxf(m, top), keep = nm == -INFINITY ? 0.f : ex2(m - nm);
-                    m = nm;
-                    l *= keep;
-                    if (t > p.first) {
-                        float o[32];
-#pragma unroll 1
-                        for (int c = 0; c < DH; c += 32) {
-                            tm_ld32(O + c, o);
-                            tm_wait_ld();
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] *= keep;
-                            tm_st32(O + c, o);
-                        }
-                    }
-                }
-                const float base = m == -INFINITY ? 0.f : m;
-                float sums[4] = {0.f, 0.f, 0.f, 0.f};
-                auto weights = [&](float (&s)[32], int col) {
-                    uint32_t u[16];
+                const unsigned lost_groups = bars.lost[(run_tiles + (t - p.first)) & 7];
+                const bool edge = (t + 1) * CH_KEYS > p.see[half];
+                u64 sums[2] = {0ull, 0ull};
+                auto weights = [&](float (&s)[32], int col, u64 less) {
+                    uint32_t w16[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        const float e0 = ex2(fmaf(s[2 * j], to_log2, -base)), e1 = ex2(fmaf(s[2 * j + 1], to_log2, -base));
-                        sums[2 * (j & 1)] += e0; sums[2 * (j & 1) + 1] += e1;
-                        u[j] = pack_bf16(e0, e1);
+                        const u64 e = fma2(two(s[2 * j], s[2 * j + 1]), by, less);
+                        const float e0 = ex2(low(e)), e1 = ex2(high(e));
+                        sums[j & 1] = add2(sums[j & 1], two(e0, e1));
+                        w16[j] = pack_bf16(e0, e1);
                     }
-                    tm_st16(S + col, u);
+                    tm_st16(S + col, w16);
                 };
-                weights(x, 0);
-                weights(y, 16);
-                tm_ld32(S + 64, x);
-                tm_ld32(S + 96, y);
-                tm_wait_ld();
-                if (edge) { mask(x, 64); mask(y, 96); }
-                weights(x, 32);
-                weights(y, 48);
-                l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
-                tm_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.pready[half]);
+                // 64 positions, then the others: when the first are out, their product with the values begins
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    tm_wait_ld();
+                    if (edge) {
+                        const int sees = lim - t * CH_KEYS - 64 * part;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            x[j] = j < sees ? x[j] : -INFINITY;
+                            y[j] = j + 32 < sees ? y[j] : -INFINITY;
+                        }
+                    }
+                    const unsigned lost = lost_groups >> (4 * part) & 15u;
+                    if (lost)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            if (lost >> (j >> 4) & 1) x[j] = -INFINITY;
+                            if (lost >> (2 + (j >> 4)) & 1) y[j] = -INFINITY;
+                        }
+                    float tops[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) tops[j] = fmaxf(x[j], y[j]);
+#pragma unroll
+                    for (int j = 4; j < 32; ++j) tops[j & 3] = max3(tops[j & 3], x[j], y[j]);
+                    const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * to_log2;     // (the scale is positive here)
+                    if (__any_sync(0xffffffffu, top > m + CH_LATE)) {
+                        const float nm = fmaxf(m, top), keep = nm == -INFINITY ? 0.f : ex2(m - nm);
+                        m = nm;
+                        l = (l + (low(sums[0]) + high(sums[0])) + (low(sums[1]) + high(sums[1]))) * keep;
+                        sums[0] = sums[1] = 0ull;
+                        if (t > p.first || part) {
+                            // (the first half's product may be under way; with the scores here, the tile before is done)
+                            if (part) ok = warp_waits(&bars.firsthalf[half], done & 1u);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < DH; c += 16) {
+                                float o[16];
+                                tc_ld16(O + c, o);
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) o[j] *= keep;
+                                tm_st16(O + c, o);
+                            }
+                        }
+                    }
+                    const float base = m == -INFINITY ? 0.f : m;
+                    const u64 less = two(-base, -base);
+                    weights(x, 32 * part, less);
+                    if (part == 0) tm_ld32(S + 64, x);
+                    weights(y, 32 * part + 16, less);
+                    if (part == 0) tm_ld32(S + 96, y);
+                    tm_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars.pready[half][part]);
+                }
+                if (!ok) break;
+                const u64 sum = add2(sums[0], sums[1]);
+                l += low(sum) + high(sum);
             }
             if (!ok) break;
             // ---- the rows leave, finished or as a part of their item
@@ -522,11 +574,32 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             float* part = a.parts + ((size_t)blockIdx.x * 2 + (p.first == 0 ? 1 : 0)) * C::PART;
             const size_t dst = mine ? (size_t)(at.q.start + token) * a.ldo + (size_t)(at.h * group + p_row % group) * DH : 0;
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            auto store_row = [&](size_t to, const float (&o)[32], float f) {
+            // 32 columns of the warp's rows: four lanes exchange 16-byte pieces, so that a store covers 64 bytes of each of eight rows
+            // instead of 16 of 32
+            auto store_rows = [&](int c, const float (&o)[32], float f) {
+                uint32_t u[4][4];
 #pragma unroll
-                for (int j = 0; j < 32; j += 8)
-                    *reinterpret_cast<uint4*>((uint16_t*)a.out + to + j) = make_uint4(pack_bf16(o[j] * f, o[j + 1] * f), pack_bf16(o[j + 2] * f, o[j + 3] * f),
-                                                                                      pack_bf16(o[j + 4] * f, o[j + 5] * f), pack_bf16(o[j + 6] * f, o[j + 7] * f));
+                for (int j = 0; j < 16; ++j) u[j >> 2][j & 3] = pack_bf16(o[2 * j] * f, o[2 * j + 1] * f);
+#pragma unroll
+                for (int d = 1; d < 4; d <<= 1)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (k & d) continue;             // pieces k and k + d: one goes over, the other stays
+                        const bool upper = lane & d;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? u[k][e] : u[k + d][e], d);
+                            if (upper) u[k][e] = got; else u[k + d][e] = got;
+                        }
+                    }
+                // u[k]: piece lane & 3 of row (lane & ~3) + k
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int from = (lane & ~3) + k;
+                    const size_t to = __shfl_sync(0xffffffffu, (u64)dst, from);
+                    if (__shfl_sync(0xffffffffu, (int)mine, from))
+                        *reinterpret_cast<uint4*>((uint16_t*)a.out + to + c + 8 * (lane & 3)) = make_uint4(u[k][0], u[k][1], u[k][2], u[k][3]);
+                }
             };
             if (any) {
 #pragma unroll 1
@@ -534,8 +607,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                     float o[32];
                     tm_ld32(O + c, o);
                     tm_wait_ld();
-                    if (!mine) continue;
-                    if (odd)                                     // infinities and NaN that this row sees
+                    if (odd && mine)                             // infinities and NaN that this row sees
                         for (int pos = max(p.see[0], p.first * CH_KEYS); pos < min(lim, p.stop * CH_KEYS); ++pos) {
                             const int pg = paged_page(w, at.s, pos);
                             const size_t row = pg >= 0 ? paged_row(w, pg, at.h, pos) : 0;
@@ -547,8 +619,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                             }
                         }
                     if (p.whole) {
-                        store_row(dst + c, o, inv);
-                    } else {
+                        store_rows(c, o, inv);
+                    } else if (mine) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) __stcg(part + (half * DH + c + j) * 128 + 32 * quad + lane, o[j]);
                     }
@@ -560,7 +632,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             if (!p.whole && p.nrows > 128 * half) {
                 if (mine) { __stcg(part + CH_ROWS * DH + r, m); __stcg(part + CH_ROWS * DH + CH_ROWS + r, l); }
                 // the half's last part to arrive adds them up, in the order of their runs
-                const int c0 = run_of(at.item_first, units, n_runs), c1 = run_of(at.item_first + at.tiles - 1, units, n_runs);
+                int c0, c1;
+                ChunkSchedule::parts_of(at, units, n_runs, snap, &c0, &c1);
                 __threadfence();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars.joined[half]);
@@ -585,22 +658,26 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                         top = base;
                     }
                     const float scale = total == 0.f ? 0.f : 1.f / total;
-                    if (mine) {
 #pragma unroll 1
-                        for (int c = 0; c < DH; c += 32) {
-                            float o[32];
+                    for (int c = 0; c < DH; c += 32) {
+                        float o[32];
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] = 0.f;
-                            for (int k = c0; k <= c1; ++k) {
-                                const float pm = __ldcg(of(k) + CH_ROWS * DH + r);
-                                if (pm == -INFINITY) continue;   // (nothing was written of the row)
-                                const float f = ex2(pm - top);
-                                const float* src = of(k) + (half * DH + c) * 128 + 32 * quad + lane;
+                        for (int j = 0; j < 32; ++j) o[j] = 0.f;
+                        float next_m = mine ? __ldcg(of(c0) + CH_ROWS * DH + r) : -INFINITY;
+#pragma unroll 1
+                        for (int k = c0; k <= c1; ++k) {
+                            const float pm = next_m;
+                            if (k < c1 && mine) next_m = __ldcg(of(k + 1) + CH_ROWS * DH + r);
+                            if (pm == -INFINITY) continue;       // (nothing was written of the row)
+                            const float* src = of(k) + (half * DH + c) * 128 + 32 * quad + lane;
+                            float x[32];
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) o[j] = fmaf(f, __ldcg(src + j * 128), o[j]);
-                            }
-                            store_row(dst + c, o, scale);
+                            for (int j = 0; j < 32; ++j) x[j] = __ldcg(src + j * 128);
+                            const float f = ex2(pm - top);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) o[j] = fmaf(f, x[j], o[j]);
                         }
+                        store_rows(c, o, scale);
                     }
                 }
             }
@@ -632,7 +709,7 @@ template <int DH, bool E4M3> static csd_status run_chunk(const PagedView& w, con
         if (!encode_map_2d(w.k, rows, DH, 1 << w.page_shift, &tk) || !encode_map_2d(w.v, rows, DH, 1 << w.page_shift, &tv)) return CSD_ERR_UNSUPPORTED;
     }
     PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(CH_THREADS), C::SMEM, st);
-    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, tk, tv, w, a, 1));
+    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, tk, tv, w, a, 1, 2));
     count_launch();
     return CSD_OK;
 }

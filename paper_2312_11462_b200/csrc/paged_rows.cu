@@ -66,7 +66,7 @@ template <int RB> __device__ __forceinline__ uint32_t stage_off(int j, int c) {
 
 template <int DH, int MT, bool ROWS16, bool E4M3>
 __global__ void __launch_bounds__(32 * PW, 1)
-paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units) {
+paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int snap) {
     using C = PagedRowsCfg<DH, MT, ROWS16, E4M3>;
     using S = Schedule<C::BR, PKEYS>;
     constexpr int BR = C::BR, KS = DH / 16, NS = C::STAGES;
@@ -89,12 +89,12 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units) {
     const u64 most = units / (unsigned)least_units;
     const unsigned n_runs = most < 1 ? 1u : most < gridDim.x ? (unsigned)most : gridDim.x;
     if (blockIdx.x >= n_runs || units == 0) return;
-    const u64 begin = run_begin(blockIdx.x, units, n_runs), end = run_begin(blockIdx.x + 1, units, n_runs);
     const bool tree = a.tree != nullptr;
     const float to_log2 = a.scale * 1.4426950408889634f;
 
     typename S::Cursor ld, at;                           // the tile to request next, the tile to multiply
-    at.seek(w, prefix, begin, a.group, tree);
+    u64 begin, end;
+    if (!S::run(w, prefix, blockIdx.x, n_runs, snap, a.group, tree, &begin, &end, &at)) return;
     ld = at;
     u64 requested = begin;
     unsigned lost = 0;                                   // stages whose page does not exist
@@ -482,7 +482,8 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units) {
         }
         if (!whole) {
             // ---- the last of the item's parts to arrive adds them up, in the order of their runs
-            const int c0 = run_of(at.item_first, units, n_runs), c1 = run_of(item_end - 1, units, n_runs);
+            int c0, c1;
+            S::parts_of(at, units, n_runs, snap, &c0, &c1);
             __threadfence();
             __syncthreads();
             if (tid == 0) s_last = atomicInc(a.tickets + c0, (unsigned)(c1 - c0)) == (unsigned)(c1 - c0);
@@ -530,7 +531,7 @@ static csd_status run_rows(const PagedView& w, const AttendArgs& a, cudaStream_t
     const csd_status ok = allow_smem(ready, kern, C::SMEM);
     if (ok != CSD_OK) return ok;
     PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(32 * PW), C::SMEM, st);
-    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a, 1));
+    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a, 1, 0));
     count_launch();
     return CSD_OK;
 }
