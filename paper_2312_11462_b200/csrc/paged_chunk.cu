@@ -498,8 +498,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                     tm_st16(S + col, w16);
                 };
                 // 64 positions, then the others: when the first are out, their product with the values begins
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
+#pragma unroll 1
+                for (int part = 0; part < 2; ++part) {           // (one copy of the code: two do not fit the schedulers' instruction caches)
                     tm_wait_ld();
                     if (edge) {
                         const int sees = lim - t * CH_KEYS - 64 * part;
