@@ -98,25 +98,33 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
     ld = at;
     u64 requested = begin;
     unsigned lost = 0;                                   // stages whose page does not exist
-    // Requests this warp's 16 positions of the tile at ld into a stage.
+    // Page of this warp's 16 positions of the tile at ld, looked up a request ahead (what is found is checked when it is used)
+    auto look_up = [&]() {
+        const int t0 = ld.tile * PKEYS + 16 * warp;
+        return t0 < ld.seen ? w.table[(size_t)ld.s * w.max_pages + (t0 >> w.page_shift)] : -1;
+    };
+    int page = look_up();
+    // Requests the positions of the tile at ld into a stage.
     auto request = [&](int slot) {
         if (requested < end) {
             const int t0 = ld.tile * PKEYS + 16 * warp, n = ld.seen - t0;
-            const int page = n > 0 ? paged_page(w, ld.s, t0) : -1;
-            if (page < 0) lost |= 1u << slot; else lost &= ~(1u << slot);
-            const size_t row = page < 0 ? 0 : paged_row(w, page, ld.h, t0);
+            const bool is = page >= 0 && page < w.n_pages;
+            if (n > 0 && !is) set_status(w.status, CSD_ERR_BAD_PAGE);
+            if (is) lost &= ~(1u << slot); else lost |= 1u << slot;
+            const size_t row = is ? paged_row(w, page, ld.h, t0) : 0;
             const uint32_t dst = st0 + slot * C::STAGE;
-            const unsigned char* ks = w.k + row * C::RB;
-            const unsigned char* vs = w.v + row * C::RB;
+            const unsigned char* ks = w.k + row * C::RB + lane * 16;
+            const unsigned char* vs = w.v + row * C::RB + lane * 16;
+            constexpr int PER = C::RB / 16;              // 16-byte chunks of a row
 #pragma unroll
             for (int i = 0; i < C::RB / 32; ++i) {
-                const int c = i * 32 + lane, j = c / (C::RB / 16), cc = c % (C::RB / 16);
-                const bool there = page >= 0 && j < n;
-                cp_async16(dst + stage_off<C::RB>(j, cc), ks + c * 16, there);
-                cp_async16(dst + 16 * C::RB + stage_off<C::RB>(j, cc), vs + c * 16, there);
+                const int c = i * 32 + lane, j = c / PER, cc = c % PER;
+                const bool there = is && j < n;
+                cp_async16(dst + stage_off<C::RB>(j, cc), ks + i * 512, there);
+                cp_async16(dst + 16 * C::RB + stage_off<C::RB>(j, cc), vs + i * 512, there);
             }
-            if (E4M3 && lane < 2) cp_async16(dst + 32 * C::RB + 16 * lane, (lane ? w.v_exp : w.k_exp) + row, page >= 0);
-            if (++requested < end) ld.next(w, a.group, tree);
+            if (E4M3 && lane < 2) cp_async16(dst + 32 * C::RB + 16 * lane, (lane ? w.v_exp : w.k_exp) + row, is);
+            if (++requested < end) { ld.next(w, a.group, tree); page = look_up(); }
         }
         cp_async_commit();
     };
@@ -219,11 +227,13 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
             request(slot == 0 ? NS - 1 : slot - 1);
             if (t0 < at.seen && !gone) {
                 // ---- scores: 16 rows a block against the warp's 16 positions, the smallest terms first
-                float s[MT][2][4];
+                float s[MT][2][4], s2[MT][2][4];         // two chains: even and odd steps of 16 dimensions
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) s[mt][g][0] = s[mt][g][1] = s[mt][g][2] = s[mt][g][3] = 0.f;
+                    for (int g = 0; g < 2; ++g)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[mt][g][e] = s2[mt][g][e] = 0.f;
 #pragma unroll
                 for (int k2 = 0; k2 < KS; k2 += 2) {
                     uint32_t kb[2][4];                   // [16 dimensions][keys 0-7: two halves, keys 8-15: two halves]
@@ -252,8 +262,9 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                                 ldsm_x4(qs0 + t * BR * DH * 2 + stage_off<2 * DH>(16 * mt + (lane & 15), 2 * (k2 + u) + (lane >> 4)), qa);
 #pragma unroll
                                 for (int g = 0; g < 2; ++g) {
-                                    if constexpr (E4M3) mma_f16(s[mt][g], qa, kb[u][2 * g], kb[u][2 * g + 1]);
-                                    else mma_bf16(s[mt][g], qa, kb[u][2 * g], kb[u][2 * g + 1]);
+                                    float (&acc)[4] = u ? s2[mt][g] : s[mt][g];
+                                    if constexpr (E4M3) mma_f16(acc, qa, kb[u][2 * g], kb[u][2 * g + 1]);
+                                    else mma_bf16(acc, qa, kb[u][2 * g], kb[u][2 * g + 1]);
                                 }
                             }
                 }
@@ -282,6 +293,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 float& x = s[mt][g][2 * hr + e];
+                                x += s2[mt][g][2 * hr + e];
                                 if constexpr (E4M3) x *= kscale[g][e];
                                 x *= q_scale[mt][hr];
                                 if (edge) {
