@@ -98,16 +98,18 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
     ld = at;
     u64 requested = begin;
     unsigned lost = 0;                                   // stages whose page does not exist
-    // Page of this warp's 16 positions of the tile at ld, looked up a request ahead (what is found is checked when it is used)
+    // Pages of this warp's 16 positions, a lane a tile: of tiles paged .. paged + 31 of the item at ld (what is found is checked when it is used)
+    int pages = -1, paged = 0;
     auto look_up = [&]() {
-        const int t0 = ld.tile * PKEYS + 16 * warp;
-        return t0 < ld.seen ? w.table[(size_t)ld.s * w.max_pages + (t0 >> w.page_shift)] : -1;
+        paged = ld.tile;
+        const int t0 = (ld.tile + lane) * PKEYS + 16 * warp;
+        pages = t0 < ld.seen ? w.table[(size_t)ld.s * w.max_pages + (t0 >> w.page_shift)] : -1;
     };
-    int page = look_up();
+    look_up();
     // Requests the positions of the tile at ld into a stage.
     auto request = [&](int slot) {
         if (requested < end) {
-            const int t0 = ld.tile * PKEYS + 16 * warp, n = ld.seen - t0;
+            const int t0 = ld.tile * PKEYS + 16 * warp, n = ld.seen - t0, page = __shfl_sync(0xffffffffu, pages, ld.tile - paged);
             const bool is = page >= 0 && page < w.n_pages;
             if (n > 0 && !is) set_status(w.status, CSD_ERR_BAD_PAGE);
             if (is) lost &= ~(1u << slot); else lost |= 1u << slot;
@@ -124,7 +126,10 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                 cp_async16(dst + 16 * C::RB + stage_off<C::RB>(j, cc), vs + i * 512, there);
             }
             if (E4M3 && lane < 2) cp_async16(dst + 32 * C::RB + 16 * lane, (lane ? w.v_exp : w.k_exp) + row, is);
-            if (++requested < end) { ld.next(w, a.group, tree); page = look_up(); }
+            if (++requested < end) {
+                ld.next(w, a.group, tree);
+                if (ld.tile == 0 || ld.tile == paged + 32) look_up();
+            }
         }
         cp_async_commit();
     };
@@ -453,45 +458,53 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
             if constexpr (ROWS16) *reinterpret_cast<uint2*>((uint16_t*)a.out + dst) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
             else *reinterpret_cast<float4*>((float*)a.out + dst) = v;
         };
+        // `dims` dimensions at a time through `buf` ([warp][row][dims])
+        auto add_up = [&](float* buf, auto dims) {
+            constexpr int MC = decltype(dims)::value;
 #pragma unroll
-        for (int d0 = 0; d0 < DH; d0 += C::MC) {
+            for (int d0 = 0; d0 < DH; d0 += MC) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+                for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                for (int hr = 0; hr < 2; ++hr) {
-                    const int r = 16 * mt + (lane >> 2) + 8 * hr;
-                    const float f = row_m[warp * BR + r];
-                    float* dst = merge + (warp * BR + r) * C::MC;
+                    for (int hr = 0; hr < 2; ++hr) {
+                        const int r = 16 * mt + (lane >> 2) + 8 * hr;
+                        const float f = row_m[warp * BR + r];
+                        float* dst = buf + (warp * BR + r) * MC;
 #pragma unroll
-                    for (int t = d0 / 8; t < (d0 + C::MC) / 8; t += 2) {
-                        const float a0 = o[mt][t][2 * hr] * f, a1 = o[mt][t][2 * hr + 1] * f, b0 = o[mt][t + 1][2 * hr] * f, b1 = o[mt][t + 1][2 * hr + 1] * f;
-                        if constexpr (E4M3) {            // (accumulators t and t + 1: the even and the odd ones of 16)
-                            *reinterpret_cast<float4*>(dst + 8 * t - d0 + 4 * (lane & 3)) = make_float4(a0, b0, a1, b1);
-                        } else {
-                            *reinterpret_cast<float2*>(dst + 8 * t - d0 + 2 * (lane & 3)) = make_float2(a0, a1);
-                            *reinterpret_cast<float2*>(dst + 8 * t + 8 - d0 + 2 * (lane & 3)) = make_float2(b0, b1);
+                        for (int t = d0 / 8; t < (d0 + MC) / 8; t += 2) {
+                            const float a0 = o[mt][t][2 * hr] * f, a1 = o[mt][t][2 * hr + 1] * f, b0 = o[mt][t + 1][2 * hr] * f, b1 = o[mt][t + 1][2 * hr + 1] * f;
+                            if constexpr (E4M3) {        // (accumulators t and t + 1: the even and the odd ones of 16)
+                                *reinterpret_cast<float4*>(dst + 8 * t - d0 + 4 * (lane & 3)) = make_float4(a0, b0, a1, b1);
+                            } else {
+                                *reinterpret_cast<float2*>(dst + 8 * t - d0 + 2 * (lane & 3)) = make_float2(a0, a1);
+                                *reinterpret_cast<float2*>(dst + 8 * t + 8 - d0 + 2 * (lane & 3)) = make_float2(b0, b1);
+                            }
                         }
                     }
-                }
-            __syncthreads();
-            constexpr int PER = C::MC / 4;
-            for (int i = tid; i < nrows * PER; i += 32 * PW) {
-                const int r = i / PER, c = i % PER * 4;
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                __syncthreads();
+                constexpr int PER = MC / 4;
+                for (int i = tid; i < nrows * PER; i += 32 * PW) {
+                    const int r = i / PER, c = i % PER * 4;
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int j = 0; j < PW; ++j) {
-                    const float4 x = *reinterpret_cast<const float4*>(merge + (j * BR + r) * C::MC + c);
-                    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+                    for (int j = 0; j < PW; ++j) {
+                        const float4 x = *reinterpret_cast<const float4*>(buf + (j * BR + r) * MC + c);
+                        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+                    }
+                    if (whole) {
+                        const float f = row_f[r];
+                        put(r, d0 + c, make_float4(v.x * f, v.y * f, v.z * f, v.w * f));
+                    } else {
+                        __stcg(reinterpret_cast<float4*>(part + r * DH + d0 + c), v);
+                    }
                 }
-                if (whole) {
-                    const float f = row_f[r];
-                    put(r, d0 + c, make_float4(v.x * f, v.y * f, v.z * f, v.w * f));
-                } else {
-                    __stcg(reinterpret_cast<float4*>(part + r * DH + d0 + c), v);
-                }
+                if (d0 + MC < DH) __syncthreads();
             }
-            __syncthreads();
-        }
+        };
+        // behind the run's last tile the stages are free for all dimensions at once
+        constexpr bool ROOM = PW * BR * DH * 4 <= NS * PW * C::STAGE;
+        if (ROOM && item_end >= end) add_up(reinterpret_cast<float*>(smem + C::FIXED), std::integral_constant<int, ROOM ? DH : C::MC>());
+        else add_up(merge, std::integral_constant<int, C::MC>());
         if (!whole) {
             // ---- the last of the item's parts to arrive adds them up, in the order of their runs
             int c0, c1;
@@ -503,26 +516,49 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
             if (s_last) {
                 __threadfence();
                 auto of = [&](int c) { return a.parts + ((size_t)c * 2 + (c == c0 ? 1 : 0)) * C::PART; };
-                for (int r = tid; r < nrows; r += 32 * PW) {
+                const int n_parts = c1 - c0 + 1;
+                // a warp a row, a lane a part: the row's maximum and sum; then what each part counts, in `merge`
+                constexpr int MOST = C::MERGE / 4 / BR;          // parts at a time
+                for (int r = warp; r < nrows; r += PW) {
                     float top = -INFINITY, sum = 0.f;
-                    for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(of(c) + BR * DH + r));
-                    if (top > -INFINITY || top != top)
-                        for (int c = c0; c <= c1; ++c) sum += exp2f(__ldcg(of(c) + BR * DH + r) - top) * __ldcg(of(c) + BR * DH + BR + r);
-                    row_f[r] = sum == 0.f ? 0.f : 1.f / sum;
-                    row_f[BR + r] = top == -INFINITY ? 0.f : top;
-                }
-                __syncthreads();
-                for (int i = tid; i < nrows * (DH / 4); i += 32 * PW) {
-                    const int r = i / (DH / 4), d = i % (DH / 4) * 4;
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                    const float top = row_f[BR + r], inv = row_f[r];
-#pragma unroll 4
-                    for (int c = c0; c <= c1; ++c) {
-                        const float f = exp2f(__ldcg(of(c) + BR * DH + r) - top);
-                        const float4 x = __ldcg(reinterpret_cast<const float4*>(of(c) + r * DH + d));
-                        v.x += f * x.x; v.y += f * x.y; v.z += f * x.z; v.w += f * x.w;
+                    for (int c = lane; c < n_parts; c += 32) top = fmaxf(top, __ldcg(of(c0 + c) + BR * DH + r));
+                    top = warp_max(top);
+                    if (top == -INFINITY) top = 0.f;
+                    for (int c = lane; c < n_parts; c += 32) sum += exp2f(__ldcg(of(c0 + c) + BR * DH + r) - top) * __ldcg(of(c0 + c) + BR * DH + BR + r);
+                    sum = warp_sum(sum);
+                    if (lane == 0) {
+                        row_f[r] = sum == 0.f ? 0.f : 1.f / sum;
+                        row_f[BR + r] = top;
                     }
-                    put(r, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+                }
+                constexpr int PER = DH / 4, EACH = (BR * PER + 32 * PW - 1) / (32 * PW);
+                float4 v[EACH] = {};
+                for (int b0 = 0; b0 < n_parts; b0 += MOST) {
+                    const int nb = min(MOST, n_parts - b0);
+                    __syncthreads();
+                    for (int i = tid; i < nrows * nb; i += 32 * PW) {
+                        const int r = i / nb, c = i % nb;
+                        merge[r * MOST + c] = exp2f(__ldcg(of(c0 + b0 + c) + BR * DH + r) - row_f[BR + r]);
+                    }
+                    __syncthreads();
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e) {
+                        const int i = tid + e * 32 * PW, r = i / PER, d = i % PER * 4;
+                        if (i >= nrows * PER) continue;
+#pragma unroll 4
+                        for (int c = 0; c < nb; ++c) {
+                            const float f = merge[r * MOST + c];
+                            const float4 x = __ldcg(reinterpret_cast<const float4*>(of(c0 + b0 + c) + r * DH + d));
+                            v[e].x += f * x.x; v[e].y += f * x.y; v[e].z += f * x.z; v[e].w += f * x.w;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) {
+                    const int i = tid + e * 32 * PW, r = i / PER, d = i % PER * 4;
+                    if (i >= nrows * PER) continue;
+                    const float f = row_f[r];
+                    put(r, d, make_float4(v[e].x * f, v[e].y * f, v[e].z * f, v[e].w * f));
                 }
             }
         }
@@ -543,7 +579,7 @@ static csd_status run_rows(const PagedView& w, const AttendArgs& a, cudaStream_t
     const csd_status ok = allow_smem(ready, kern, C::SMEM);
     if (ok != CSD_OK) return ok;
     PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(32 * PW), C::SMEM, st);
-    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a, 1, 0));
+    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a, 2, 2));
     count_launch();
     return CSD_OK;
 }

@@ -136,12 +136,26 @@ template <int BR, int KEYS> struct Schedule {
     // end moves there: a part costs its writing, its adding up and another start.  False: nothing is left for this CTA.
     static __device__ bool run(const PagedView& w, const u64* prefix, int c, unsigned n, int snap, int group, bool tree, u64* begin, u64* end, Cursor* at) {
         const u64 units = prefix[w.n_seqs];
+        const bool one = w.max_rows * group <= BR;       // one block a sequence: its items are alike
         auto cut = [&](int i) {
             const u64 raw = (u64)i * units / n;
             if (raw == 0 || raw >= units) return raw;
-            at->seek(w, prefix, raw, group, tree);
-            if (at->tile <= min(snap, at->tiles / 2)) return at->item_first;
-            return at->tiles - at->tile <= snap ? at->item_first + at->tiles : raw;
+            int tile, tiles;
+            if (one) {
+                int lo = 0, hi = w.n_seqs - 1;
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (prefix[mid] <= raw) lo = mid; else hi = mid - 1;
+                }
+                const unsigned all = (unsigned)(prefix[lo + 1] - prefix[lo]);        // (a sequence has fewer than 2^30 / KEYS tiles a head)
+                tiles = (int)(all / (unsigned)w.heads);
+                tile = (int)((unsigned)(raw - prefix[lo]) % (unsigned)tiles);
+            } else {
+                at->seek(w, prefix, raw, group, tree);
+                tile = at->tile; tiles = at->tiles;
+            }
+            if (tile <= min(snap, tiles / 2)) return raw - tile;
+            return tiles - tile <= snap ? raw - tile + tiles : raw;
         };
         *end = cut(c + 1);
         *begin = cut(c);
