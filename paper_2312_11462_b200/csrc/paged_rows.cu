@@ -1,8 +1,8 @@
 // Attention over the paged cache for few rows a sequence: decode, reviews of drafted blocks and trees (and fp32 rows of any number).
 //
 // What bounds it is the cache: each visible page is read once per block of 16 or 32 (row, query head) pairs.  A CTA has
-// eight warps, one CTA an SM.  A key tile is 128 positions, 16 a warp, always inside one page; each warp stages its own keys and values
-// with cp.async, several tiles ahead, across the ends of items, and never waits for another warp until an item ends: it keeps
+// eight warps, one CTA an SM.  A key tile is 128 or 256 positions, one or two groups of 16 a warp, a group always inside one page; each warp
+// stages its own keys and values with cp.async, several tiles ahead, across the ends of items, and never waits for another warp until an item ends: it keeps
 // its own running maximum, sum and output, which the CTA's warps add up through shared memory.  An SM has 96 to 128 KB in flight that
 // way, twice what the memory's latency asks for.
 //
@@ -21,7 +21,7 @@
 
 namespace csd {
 
-constexpr int PW = 8, PKEYS = 16 * PW;          // warps of a CTA, positions of a key tile
+constexpr int PW = 8;                           // warps of a CTA
 constexpr int PSMEM = 227 * 1024;
 constexpr float LATE = 8.f;                     // a running maximum may lag by this power of two (weights of up to 2^8)
 
@@ -30,11 +30,14 @@ template <int DH, int MT, bool ROWS16, bool E4M3> struct PagedRowsCfg {
     static constexpr int RB = E4M3 ? DH : 2 * DH;                        // bytes of a cache row
     static constexpr int QT = ROWS16 ? 1 : E4M3 ? 2 : 3;                 // terms of a query entry
     static constexpr int PT = ROWS16 ? 1 : 3;                            // of a weight
-    static constexpr int STAGE = 2 * 16 * RB + (E4M3 ? 32 : 0);          // a warp's keys and values of a tile
-    static constexpr int MC = MT == 1 ? 32 : 16;                         // dimensions added up at a time
+    // groups of 16 positions that a warp takes of a tile: two where rows are short, whose loading time one group's chain of
+    // products, maxima and exponentials exceeds (8-bit rows of 128, 296 heads of 16384 positions: 390 us with one)
+    static constexpr int GK = RB <= 128 && (MT == 1 || ROWS16) ? 2 : 1, WK = 16 * GK, KEYS = WK * PW;
+    static constexpr int STAGE = 2 * WK * RB + (E4M3 ? 2 * WK : 0);      // a warp's keys, values and scales of a tile
+    static constexpr int MC = MT == 1 ? 32 : 16;                         // dimensions of all rows that are added up at a time
     static constexpr int PREFIX = (CSD_MAX_SEQS + 1) * 8, Q = QT * BR * DH * 2, MERGE = PW * BR * MC * 4, ROWF = (2 * PW + 3) * BR * 4;
     static constexpr int FIXED = (PREFIX + Q + MERGE + ROWF + 15) / 16 * 16;
-    static constexpr int FIT = (PSMEM - FIXED - 512) / (PW * STAGE), STAGES = FIT > 6 ? 6 : FIT;
+    static constexpr int FIT = (PSMEM - FIXED - 512) / (PW * STAGE), STAGES = FIT > 5 ? 5 : FIT;
     static_assert(STAGES >= 2, "two tiles in flight");
     static constexpr int SMEM = FIXED + STAGES * PW * STAGE;
     static constexpr int PART = BR * (DH + 2);                           // floats of a part: rows, maxima, sums
@@ -68,8 +71,8 @@ template <int DH, int MT, bool ROWS16, bool E4M3>
 __global__ void __launch_bounds__(32 * PW, 1)
 paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int snap) {
     using C = PagedRowsCfg<DH, MT, ROWS16, E4M3>;
-    using S = Schedule<C::BR, PKEYS>;
-    constexpr int BR = C::BR, KS = DH / 16, NS = C::STAGES;
+    using S = Schedule<C::BR, C::KEYS>;
+    constexpr int BR = C::BR, KS = DH / 16, NS = C::STAGES, GK = C::GK, WK = C::WK, RB = C::RB;
     extern __shared__ __align__(128) unsigned char smem[];
     u64* prefix = reinterpret_cast<u64*>(smem);
     unsigned char* Qs = smem + (C::PREFIX + 15) / 16 * 16;
@@ -97,42 +100,47 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
     if (!S::run(w, prefix, blockIdx.x, n_runs, snap, a.group, tree, &begin, &end, &at)) return;
     ld = at;
     u64 requested = begin;
-    unsigned lost = 0;                                   // stages whose page does not exist
-    // Pages of this warp's 16 positions, a lane a tile: of tiles paged .. paged + 31 of the item at ld (what is found is checked when it is used)
+    unsigned lost = 0;                                   // GK bits a stage: groups that have no positions or no page
+    // Pages of this warp's groups, a lane a group: of tiles paged .. of the item at ld (what is found is checked when it is used)
     int pages = -1, paged = 0;
     auto look_up = [&]() {
         paged = ld.tile;
-        const int t0 = (ld.tile + lane) * PKEYS + 16 * warp;
+        const int t0 = (ld.tile + lane / GK) * C::KEYS + WK * warp + 16 * (lane % GK);
         pages = t0 < ld.seen ? w.table[(size_t)ld.s * w.max_pages + (t0 >> w.page_shift)] : -1;
     };
     look_up();
     // Requests the positions of the tile at ld into a stage.
     auto request = [&](int slot) {
         if (requested < end) {
-            const int t0 = ld.tile * PKEYS + 16 * warp, n = ld.seen - t0, page = __shfl_sync(0xffffffffu, pages, ld.tile - paged);
-            const bool is = page >= 0 && page < w.n_pages;
-            if (n > 0 && !is) set_status(w.status, CSD_ERR_BAD_PAGE);
-            if (is) lost &= ~(1u << slot); else lost |= 1u << slot;
-            const size_t row = is ? paged_row(w, page, ld.h, t0) : 0;
             const uint32_t dst = st0 + slot * C::STAGE;
-            const unsigned char* ks = w.k + row * C::RB + lane * 16;
-            const unsigned char* vs = w.v + row * C::RB + lane * 16;
-            constexpr int PER = C::RB / 16;              // 16-byte chunks of a row
+            lost &= ~(((1u << GK) - 1) << (slot * GK));
 #pragma unroll
-            for (int i = 0; i < C::RB / 32; ++i) {
-                const int c = i * 32 + lane, j = c / PER, cc = c % PER;
-                const bool there = is && j < n;
-                cp_async16(dst + stage_off<C::RB>(j, cc), ks + i * 512, there);
-                cp_async16(dst + 16 * C::RB + stage_off<C::RB>(j, cc), vs + i * 512, there);
+            for (int q = 0; q < GK; ++q) {
+                const int t0 = ld.tile * C::KEYS + WK * warp + 16 * q, n = ld.seen - t0, page = __shfl_sync(0xffffffffu, pages, (ld.tile - paged) * GK + q);
+                const bool is = page >= 0 && page < w.n_pages;
+                if (n > 0 && !is) set_status(w.status, CSD_ERR_BAD_PAGE);
+                if (!is) lost |= 1u << (slot * GK + q);
+                const size_t row = is ? paged_row(w, page, ld.h, t0) : 0;
+                const unsigned char* ks = w.k + row * RB + lane * 16;
+                const unsigned char* vs = w.v + row * RB + lane * 16;
+                constexpr int PER = RB / 16;             // 16-byte chunks of a row
+#pragma unroll
+                for (int i = 0; i < RB / 32; ++i) {
+                    const int c = i * 32 + lane, j = c / PER, cc = c % PER;
+                    const bool there = is && j < n;
+                    cp_async16(dst + stage_off<RB>(16 * q + j, cc), ks + i * 512, there);
+                    cp_async16(dst + WK * RB + stage_off<RB>(16 * q + j, cc), vs + i * 512, there);
+                }
+                if (E4M3 && lane < 2) cp_async16(dst + 2 * WK * RB + 16 * q + WK * lane, (lane ? w.v_exp : w.k_exp) + row, is);
             }
-            if (E4M3 && lane < 2) cp_async16(dst + 32 * C::RB + 16 * lane, (lane ? w.v_exp : w.k_exp) + row, is);
             if (++requested < end) {
                 ld.next(w, a.group, tree);
-                if (ld.tile == 0 || ld.tile == paged + 32) look_up();
+                if (ld.tile == 0 || ld.tile == paged + 32 / GK) look_up();
             }
         }
         cp_async_commit();
     };
+#pragma unroll 1
     for (int i = 0; i < NS - 1; ++i) request(i);
 
     int slot = 0;
@@ -226,36 +234,40 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
         for (int tile = first_tile; tile < stop; ++tile) {
             cp_async_wait<NS - 2>();
             __syncwarp();                                // the stage has landed for all lanes, and all have read the one before
-            const int t0 = tile * PKEYS + 16 * warp;
-            const uint32_t Kt = st0 + slot * C::STAGE, Vt = Kt + 16 * C::RB;
-            const bool gone = lost >> slot & 1;
+            const int t0 = tile * C::KEYS + WK * warp;
+            const uint32_t Kt = st0 + slot * C::STAGE, Vt = Kt + WK * RB;
+            const unsigned gone = lost >> (slot * GK) & ((1u << GK) - 1);
             request(slot == 0 ? NS - 1 : slot - 1);
-            if (t0 < at.seen && !gone) {
-                // ---- scores: 16 rows a block against the warp's 16 positions, the smallest terms first
-                float s[MT][2][4], s2[MT][2][4];         // two chains: even and odd steps of 16 dimensions
+            if (gone != (1u << GK) - 1) {
+                // ---- scores: 16 rows a block against the warp's positions in blocks of 8, the smallest terms first
+                constexpr int NG = 2 * GK, CH = GK == 1 ? 2 : 1;         // (of one group two chains, even and odd steps of 16 dimensions)
+                float s[MT][NG][4], more[CH][MT][NG][4];
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                    for (int g = 0; g < 2; ++g)
+                    for (int g = 0; g < NG; ++g)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[mt][g][e] = s2[mt][g][e] = 0.f;
+                        for (int e = 0; e < 4; ++e) s[mt][g][e] = more[CH - 1][mt][g][e] = 0.f;
+                const int key = (lane >> 4) * 8 + (lane & 7);
 #pragma unroll
                 for (int k2 = 0; k2 < KS; k2 += 2) {
-                    uint32_t kb[2][4];                   // [16 dimensions][keys 0-7: two halves, keys 8-15: two halves]
-                    const int key = (lane >> 4) * 8 + (lane & 7);
-                    if constexpr (E4M3) {
-                        uint32_t raw[4];
-                        ldsm_x4(Kt + stage_off<C::RB>(key, k2 + ((lane >> 3) & 1)), raw);
+                    uint32_t kb[2][GK][4];               // [16 dimensions][group][keys 0-7: two halves, keys 8-15: two halves]
 #pragma unroll
-                        for (int u = 0; u < 2; ++u)
+                    for (int q = 0; q < GK; ++q) {
+                        if constexpr (E4M3) {
+                            uint32_t raw[4];
+                            ldsm_x4(Kt + stage_off<RB>(16 * q + key, k2 + ((lane >> 3) & 1)), raw);
 #pragma unroll
-                            for (int g = 0; g < 2; ++g) {
-                                kb[u][2 * g] = e4m3_to_f16(raw[2 * g + u] & 0xffffu);
-                                kb[u][2 * g + 1] = e4m3_to_f16(raw[2 * g + u] >> 16);
-                            }
-                    } else {
+                            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) ldsm_x4(Kt + stage_off<C::RB>(key, 2 * (k2 + u) + ((lane >> 3) & 1)), kb[u]);
+                                for (int g = 0; g < 2; ++g) {
+                                    kb[u][q][2 * g] = e4m3_to_f16(raw[2 * g + u] & 0xffffu);
+                                    kb[u][q][2 * g + 1] = e4m3_to_f16(raw[2 * g + u] >> 16);
+                                }
+                        } else {
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) ldsm_x4(Kt + stage_off<RB>(16 * q + key, 2 * (k2 + u) + ((lane >> 3) & 1)), kb[u][q]);
+                        }
                     }
 #pragma unroll
                     for (int t = C::QT - 1; t >= 0; --t)
@@ -266,48 +278,50 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                                 uint32_t qa[4];
                                 ldsm_x4(qs0 + t * BR * DH * 2 + stage_off<2 * DH>(16 * mt + (lane & 15), 2 * (k2 + u) + (lane >> 4)), qa);
 #pragma unroll
-                                for (int g = 0; g < 2; ++g) {
-                                    float (&acc)[4] = u ? s2[mt][g] : s[mt][g];
-                                    if constexpr (E4M3) mma_f16(acc, qa, kb[u][2 * g], kb[u][2 * g + 1]);
-                                    else mma_bf16(acc, qa, kb[u][2 * g], kb[u][2 * g + 1]);
+                                for (int g = 0; g < NG; ++g) {
+                                    float (&acc)[4] = CH == 2 && u ? more[CH - 1][mt][g] : s[mt][g];
+                                    const uint32_t (&kk)[4] = kb[u][g >> 1];
+                                    if constexpr (E4M3) mma_f16(acc, qa, kk[2 * (g & 1)], kk[2 * (g & 1) + 1]);
+                                    else mma_bf16(acc, qa, kk[2 * (g & 1)], kk[2 * (g & 1) + 1]);
                                 }
                             }
                 }
-                float kscale[2][2], vscale[2][2];        // [keys 0-7, 8-15][this lane's two]
+                float kscale[NG][2], vscale[NG][2];      // [8 keys][this lane's two]
                 if constexpr (E4M3) {
-                    const unsigned char* ex = stages + slot * C::STAGE + 32 * C::RB;
+                    const unsigned char* ex = stages + slot * C::STAGE + 2 * WK * RB;
 #pragma unroll
-                    for (int g = 0; g < 2; ++g) {
+                    for (int g = 0; g < NG; ++g) {
                         const uint32_t ke = *reinterpret_cast<const uint16_t*>(ex + 8 * g + 2 * (lane & 3));
-                        const uint32_t ve = *reinterpret_cast<const uint16_t*>(ex + 16 + 8 * g + 2 * (lane & 3));
+                        const uint32_t ve = *reinterpret_cast<const uint16_t*>(ex + WK + 8 * g + 2 * (lane & 3));
                         kscale[g][0] = row_scale(ke & 255u); kscale[g][1] = row_scale(ke >> 8);
                         vscale[g][0] = row_scale(ve & 255u); vscale[g][1] = row_scale(ve >> 8);
                     }
                 }
                 // ---- scale and mask; the warp's own running maxima
-                const bool edge = t0 + 16 > all_see;
+                const bool edge = t0 + WK > all_see || gone;
                 float mx[MT][2];
                 bool grown = false;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                     for (int hr = 0; hr < 2; ++hr) {
-                        float top = -INFINITY;
 #pragma unroll
-                        for (int g = 0; g < 2; ++g)
+                        for (int g = 0; g < NG; ++g)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 float& x = s[mt][g][2 * hr + e];
-                                x += s2[mt][g][2 * hr + e];
+                                if constexpr (CH == 2) x += more[CH - 1][mt][g][2 * hr + e];
                                 if constexpr (E4M3) x *= kscale[g][e];
                                 x *= q_scale[mt][hr];
                                 if (edge) {
                                     const int t = t0 + 8 * g + 2 * (lane & 3) + e, back = t - at.q.kv;
                                     const bool sees = t < lim[mt][hr] || (back >= 0 && back < 64 && t < at.seen && (bits[mt][hr] >> back & 1));
-                                    if (!sees) x = -INFINITY;
+                                    if (!sees || (gone >> (g >> 1) & 1)) x = -INFINITY;
                                 }
-                                top = fmaxf(top, x);
                             }
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) top = fmaxf(top, fmaxf(s[mt][g][2 * hr], s[mt][g][2 * hr + 1]));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                         mx[mt][hr] = top;
@@ -319,7 +333,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
 #pragma unroll
                         for (int hr = 0; hr < 2; ++hr) {
                             const float nm = fmaxf(m[mt][hr], mx[mt][hr]);
-                            const float keep = nm == -INFINITY ? 0.f : exp2f(m[mt][hr] - nm);
+                            const float keep = nm == -INFINITY ? 0.f : ex2(m[mt][hr] - nm);
                             m[mt][hr] = nm;
                             l[mt][hr] *= keep;
 #pragma unroll
@@ -327,97 +341,105 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                         }
                 }
                 // ---- weights as operand rows; the sums run over the weights as the products see them
-                uint32_t pa[MT][C::PT][4];
+                uint32_t pa[MT][GK][C::PT][4];
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                    for (int f = 0; f < 4; ++f) {                        // rows lane / 4 + 8 (f & 1), keys 8 (f >> 1) + this lane's two
-                        const int hr = f & 1, g = f >> 1;
-                        const float base = m[mt][hr] == -INFINITY ? 0.f : m[mt][hr];
-                        float x = exp2f(s[mt][g][2 * hr] - base), y = exp2f(s[mt][g][2 * hr + 1] - base), x0 = x, y0 = y;
-                        float sum = 0.f;
+                    for (int q = 0; q < GK; ++q)
 #pragma unroll
-                        for (int t = 0; t < C::PT; ++t) {
-                            uint32_t u = pack_bf16(x, y);
-                            const float xr = bf16lo(u), yr = bf16hi(u);
-                            x -= xr; y -= yr;
-                            sum += xr + yr;
-                            if constexpr (E4M3) {
+                        for (int f = 0; f < 4; ++f) {                    // rows lane / 4 + 8 (f & 1), keys 8 (f >> 1) + this lane's two
+                            const int hr = f & 1, g = 2 * q + (f >> 1);
+                            const float base = m[mt][hr] == -INFINITY ? 0.f : m[mt][hr];
+                            const float x0 = ex2(s[mt][g][2 * hr] - base), y0 = ex2(s[mt][g][2 * hr + 1] - base);
+                            float x = x0, y = y0, sum = 0.f;
+#pragma unroll
+                            for (int t = 0; t < C::PT; ++t) {
+                                uint32_t u = pack_bf16(x, y);
+                                const float xr = bf16lo(u), yr = bf16hi(u);
+                                x -= xr; y -= yr;
+                                sum += xr + yr;
                                 // (a power of two: exact; a position that nobody sees may have any scale)
-                                u = pack_bf16(x0 == 0.f ? 0.f : xr * vscale[g][0], y0 == 0.f ? 0.f : yr * vscale[g][1]);
+                                if constexpr (E4M3) u = pack_bf16(x0 == 0.f ? 0.f : xr * vscale[g][0], y0 == 0.f ? 0.f : yr * vscale[g][1]);
+                                pa[mt][q][t][f] = u;
                             }
-                            pa[mt][t][f] = u;
+                            l[mt][hr] += sum;
                         }
-                        l[mt][hr] += sum;
-                    }
                 // ---- output += weights . values.  0 x NaN is NaN: where some rows do not see all of the positions, infinities and NaN
                 //      among their values send the warp through them one by one (fp32 rows everywhere: an infinity times a weight's
                 //      terms is one less another)
                 bool odd = false;
                 if (edge || !ROWS16) {
-                    const int key = lane >> 1;
                     if constexpr (E4M3) {
-                        odd = t0 + key < at.seen && (stages + slot * C::STAGE + 32 * C::RB)[16 + key] == 255u;
+                        odd = lane < WK && t0 + lane < at.seen && (stages + slot * C::STAGE + 2 * WK * RB)[WK + lane] == 255u;
                     } else {
 #pragma unroll
-                        for (int i = 0; i < C::RB / 32; ++i) {
-                            const uint4 u = *reinterpret_cast<const uint4*>(stages + slot * C::STAGE + 16 * C::RB + key * C::RB + ((2 * i + (lane & 1)) << 4));
+                        for (int i = 0; i < WK * RB / 512; ++i) {
+                            const uint4 u = *reinterpret_cast<const uint4*>(stages + slot * C::STAGE + WK * RB + (i * 32 + lane) * 16);
                             odd |= odd_bf16(u.x) || odd_bf16(u.y) || odd_bf16(u.z) || odd_bf16(u.w);
                         }
                     }
                 }
                 if (__any_sync(0xffffffffu, odd)) {
-                    const unsigned char* vt = stages + slot * C::STAGE + 16 * C::RB;
+                    const unsigned char* vt = stages + slot * C::STAGE + WK * RB;
 #pragma unroll 1
-                    for (int key = 0; key < 16; ++key) {
-                        const int from = (lane & ~3) | ((key & 7) >> 1);
-                        const float vs = E4M3 ? row_scale(vt[16 * C::RB + 16 + key]) : 1.f;
+                    for (int k = 0; k < WK; ++k) {
+                        const int from = (lane & ~3) | ((k & 7) >> 1);
+                        const float vs = E4M3 ? row_scale(vt[WK * RB + WK + k]) : 1.f;
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                             for (int hr = 0; hr < 2; ++hr) {
-                                const float a0 = key < 8 ? s[mt][0][2 * hr] : s[mt][1][2 * hr], a1 = key < 8 ? s[mt][0][2 * hr + 1] : s[mt][1][2 * hr + 1];
-                                const float x = __shfl_sync(0xffffffffu, key & 1 ? a1 : a0, from);
+                                float x = 0.f;
+#pragma unroll
+                                for (int g = 0; g < NG; ++g) {
+                                    const float even = s[mt][g][2 * hr], uneven = s[mt][g][2 * hr + 1];
+                                    x = (k & ~6) == 8 * g ? even : x;
+                                    x = (k & ~6) == 8 * g + 1 ? uneven : x;
+                                }
+                                x = __shfl_sync(0xffffffffu, x, from);
                                 if (x == -INFINITY) continue;            // (not seen)
-                                const float weight = exp2f(x - m[mt][hr]);
+                                const float weight = ex2(x - m[mt][hr]);
 #pragma unroll
                                 for (int t = 0; t < DH / 8; ++t)
 #pragma unroll
                                     for (int e = 0; e < 2; ++e) {
                                         float v;
                                         if constexpr (E4M3)
-                                            v = __half2float(__ushort_as_half((unsigned short)e4m3_to_f16(vt[stage_off<C::RB>(key, t >> 1) + 4 * (lane & 3) + 2 * e + (t & 1)]))) * vs;
+                                            v = __half2float(__ushort_as_half((unsigned short)e4m3_to_f16(vt[stage_off<RB>(k, t >> 1) + 4 * (lane & 3) + 2 * e + (t & 1)]))) * vs;
                                         else
-                                            v = bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(vt + stage_off<C::RB>(key, t) + 2 * (2 * (lane & 3) + e)));
+                                            v = bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(vt + stage_off<RB>(k, t) + 2 * (2 * (lane & 3) + e)));
                                         o[mt][t][2 * hr + e] = fmaf(weight, v, o[mt][t][2 * hr + e]);
                                     }
                             }
                     }
-                } else
+                } else {
 #pragma unroll
-                for (int j = 0; j < C::RB / 32; ++j) {
-                    uint32_t vb[4];
-                    ldsm_x4_t(Vt + stage_off<C::RB>(lane & 15, 2 * j + (lane >> 4)), vb);
-                    if constexpr (E4M3) {
+                    for (int q = 0; q < GK; ++q)
 #pragma unroll
-                        for (int u = 0; u < 2; ++u)                      // 16 dimensions, the even ones and the odd ones
+                        for (int j = 0; j < RB / 32; ++j) {
+                            uint32_t vb[4];
+                            ldsm_x4_t(Vt + stage_off<RB>(16 * q + (lane & 15), 2 * j + (lane >> 4)), vb);
+                            if constexpr (E4M3) {
 #pragma unroll
-                            for (int odd = 0; odd < 2; ++odd) {
-                                const uint32_t b0 = e4m3_to_bf16(vb[2 * u], odd), b1 = e4m3_to_bf16(vb[2 * u + 1], odd);
+                                for (int u = 0; u < 2; ++u)              // 16 dimensions, the even ones and the odd ones
+#pragma unroll
+                                    for (int b = 0; b < 2; ++b) {
+                                        const uint32_t b0 = e4m3_to_bf16(vb[2 * u], b), b1 = e4m3_to_bf16(vb[2 * u + 1], b);
+#pragma unroll
+                                        for (int t = C::PT - 1; t >= 0; --t)
+#pragma unroll
+                                            for (int mt = 0; mt < MT; ++mt) mma_bf16(o[mt][4 * j + 2 * u + b], pa[mt][q][t], b0, b1);
+                                    }
+                            } else {
 #pragma unroll
                                 for (int t = C::PT - 1; t >= 0; --t)
 #pragma unroll
-                                    for (int mt = 0; mt < MT; ++mt) mma_bf16(o[mt][4 * j + 2 * u + odd], pa[mt][t], b0, b1);
+                                    for (int mt = 0; mt < MT; ++mt) {
+                                        mma_bf16(o[mt][2 * j], pa[mt][q][t], vb[0], vb[1]);
+                                        mma_bf16(o[mt][2 * j + 1], pa[mt][q][t], vb[2], vb[3]);
+                                    }
                             }
-                    } else {
-#pragma unroll
-                        for (int t = C::PT - 1; t >= 0; --t)
-#pragma unroll
-                            for (int mt = 0; mt < MT; ++mt) {
-                                mma_bf16(o[mt][2 * j], pa[mt][t], vb[0], vb[1]);
-                                mma_bf16(o[mt][2 * j + 1], pa[mt][t], vb[2], vb[3]);
-                            }
-                    }
+                        }
                 }
             }
             slot = slot + 1 == NS ? 0 : slot + 1;
@@ -444,7 +466,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
             float top = -INFINITY, sum = 0.f;
             for (int i = 0; i < PW; ++i) top = fmaxf(top, row_m[i * BR + tid]);
             for (int i = 0; i < PW; ++i) {
-                const float f = top == -INFINITY ? 0.f : exp2f(row_m[i * BR + tid] - top);
+                const float f = top == -INFINITY ? 0.f : ex2(row_m[i * BR + tid] - top);
                 sum += f * row_l[i * BR + tid];
                 row_m[i * BR + tid] = f;                 // from here on: the warp's share of the item's rows
             }
@@ -458,53 +480,54 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
             if constexpr (ROWS16) *reinterpret_cast<uint2*>((uint16_t*)a.out + dst) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
             else *reinterpret_cast<float4*>((float*)a.out + dst) = v;
         };
-        // `dims` dimensions at a time through `buf` ([warp][row][dims])
-        auto add_up = [&](float* buf, auto dims) {
-            constexpr int MC = decltype(dims)::value;
+        // `dims` dimensions of the valid rows at a time through `buf` ([warp][row][dims]): all at once where they fit, and behind the
+        // run's last tile, when the stages are free
+        constexpr bool ROOM = PW * BR * DH * 4 <= NS * PW * C::STAGE;
+        float* buf = ROOM && item_end >= end ? reinterpret_cast<float*>(smem + C::FIXED) : merge;
+        int dims = DH;
+        if (buf == merge)
+            while (nrows * dims > BR * C::MC) dims >>= 1;
+#pragma unroll 1
+        for (int d0 = 0; d0 < DH; d0 += dims) {
 #pragma unroll
-            for (int d0 = 0; d0 < DH; d0 += MC) {
+            for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int hr = 0; hr < 2; ++hr) {
+                    const int r = 16 * mt + (lane >> 2) + 8 * hr;
+                    if (r >= nrows) continue;
+                    const float f = row_m[warp * BR + r];
+                    float* dst = buf + (warp * nrows + r) * dims - d0;
 #pragma unroll
-                    for (int hr = 0; hr < 2; ++hr) {
-                        const int r = 16 * mt + (lane >> 2) + 8 * hr;
-                        const float f = row_m[warp * BR + r];
-                        float* dst = buf + (warp * BR + r) * MC;
-#pragma unroll
-                        for (int t = d0 / 8; t < (d0 + MC) / 8; t += 2) {
-                            const float a0 = o[mt][t][2 * hr] * f, a1 = o[mt][t][2 * hr + 1] * f, b0 = o[mt][t + 1][2 * hr] * f, b1 = o[mt][t + 1][2 * hr + 1] * f;
-                            if constexpr (E4M3) {        // (accumulators t and t + 1: the even and the odd ones of 16)
-                                *reinterpret_cast<float4*>(dst + 8 * t - d0 + 4 * (lane & 3)) = make_float4(a0, b0, a1, b1);
-                            } else {
-                                *reinterpret_cast<float2*>(dst + 8 * t - d0 + 2 * (lane & 3)) = make_float2(a0, a1);
-                                *reinterpret_cast<float2*>(dst + 8 * t + 8 - d0 + 2 * (lane & 3)) = make_float2(b0, b1);
-                            }
+                    for (int t = 0; t < DH / 8; t += 2) {
+                        if (8 * t < d0 || 8 * t >= d0 + dims) continue;
+                        const float a0 = o[mt][t][2 * hr] * f, a1 = o[mt][t][2 * hr + 1] * f, b0 = o[mt][t + 1][2 * hr] * f, b1 = o[mt][t + 1][2 * hr + 1] * f;
+                        if constexpr (E4M3) {            // (accumulators t and t + 1: the even and the odd ones of 16)
+                            *reinterpret_cast<float4*>(dst + 8 * t + 4 * (lane & 3)) = make_float4(a0, b0, a1, b1);
+                        } else {
+                            *reinterpret_cast<float2*>(dst + 8 * t + 2 * (lane & 3)) = make_float2(a0, a1);
+                            *reinterpret_cast<float2*>(dst + 8 * t + 8 + 2 * (lane & 3)) = make_float2(b0, b1);
                         }
                     }
-                __syncthreads();
-                constexpr int PER = MC / 4;
-                for (int i = tid; i < nrows * PER; i += 32 * PW) {
-                    const int r = i / PER, c = i % PER * 4;
-                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int j = 0; j < PW; ++j) {
-                        const float4 x = *reinterpret_cast<const float4*>(buf + (j * BR + r) * MC + c);
-                        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-                    }
-                    if (whole) {
-                        const float f = row_f[r];
-                        put(r, d0 + c, make_float4(v.x * f, v.y * f, v.z * f, v.w * f));
-                    } else {
-                        __stcg(reinterpret_cast<float4*>(part + r * DH + d0 + c), v);
-                    }
                 }
-                if (d0 + MC < DH) __syncthreads();
+            __syncthreads();
+            const int per = dims / 4;
+            for (int i = tid; i < nrows * per; i += 32 * PW) {
+                const int r = i / per, c = i % per * 4;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int j = 0; j < PW; ++j) {
+                    const float4 x = *reinterpret_cast<const float4*>(buf + (j * nrows + r) * dims + c);
+                    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+                }
+                if (whole) {
+                    const float f = row_f[r];
+                    put(r, d0 + c, make_float4(v.x * f, v.y * f, v.z * f, v.w * f));
+                } else {
+                    __stcg(reinterpret_cast<float4*>(part + r * DH + d0 + c), v);
+                }
             }
-        };
-        // behind the run's last tile the stages are free for all dimensions at once
-        constexpr bool ROOM = PW * BR * DH * 4 <= NS * PW * C::STAGE;
-        if (ROOM && item_end >= end) add_up(reinterpret_cast<float*>(smem + C::FIXED), std::integral_constant<int, ROOM ? DH : C::MC>());
-        else add_up(merge, std::integral_constant<int, C::MC>());
+            if (d0 + dims < DH) __syncthreads();
+        }
         if (!whole) {
             // ---- the last of the item's parts to arrive adds them up, in the order of their runs
             int c0, c1;
@@ -524,7 +547,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                     for (int c = lane; c < n_parts; c += 32) top = fmaxf(top, __ldcg(of(c0 + c) + BR * DH + r));
                     top = warp_max(top);
                     if (top == -INFINITY) top = 0.f;
-                    for (int c = lane; c < n_parts; c += 32) sum += exp2f(__ldcg(of(c0 + c) + BR * DH + r) - top) * __ldcg(of(c0 + c) + BR * DH + BR + r);
+                    for (int c = lane; c < n_parts; c += 32) sum += ex2(__ldcg(of(c0 + c) + BR * DH + r) - top) * __ldcg(of(c0 + c) + BR * DH + BR + r);
                     sum = warp_sum(sum);
                     if (lane == 0) {
                         row_f[r] = sum == 0.f ? 0.f : 1.f / sum;
@@ -538,7 +561,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                     __syncthreads();
                     for (int i = tid; i < nrows * nb; i += 32 * PW) {
                         const int r = i / nb, c = i % nb;
-                        merge[r * MOST + c] = exp2f(__ldcg(of(c0 + b0 + c) + BR * DH + r) - row_f[BR + r]);
+                        merge[r * MOST + c] = ex2(__ldcg(of(c0 + b0 + c) + BR * DH + r) - row_f[BR + r]);
                     }
                     __syncthreads();
 #pragma unroll
@@ -579,7 +602,7 @@ static csd_status run_rows(const PagedView& w, const AttendArgs& a, cudaStream_t
     const csd_status ok = allow_smem(ready, kern, C::SMEM);
     if (ok != CSD_OK) return ok;
     PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(32 * PW), C::SMEM, st);
-    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a, 2, 2));
+    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a, 1, 2));
     count_launch();
     return CSD_OK;
 }
