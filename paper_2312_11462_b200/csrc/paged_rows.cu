@@ -1,10 +1,10 @@
 // Attention over the paged cache for few rows a sequence: decode, reviews of drafted blocks and trees (and fp32 rows of any number).
 //
-// What bounds it is the cache: each visible page is read once per block of 16 or 32 (row, query head) pairs.  A CTA has
-// eight warps, one CTA an SM.  A key tile is 128 or 256 positions, one or two groups of 16 a warp, a group always inside one page; each warp
+// What bounds it is the cache: each visible page is read once per block of 16 or 32 (row, query head) pairs.  A CTA has twelve
+// or eight warps, one CTA an SM.  A key tile is one or two groups of 16 positions a warp, a group always inside one page; each warp
 // stages its own keys and values with cp.async, several tiles ahead, across the ends of items, and never waits for another warp until an item ends: it keeps
 // its own running maximum, sum and output, which the CTA's warps add up through shared memory.  An SM has 96 to 128 KB in flight that
-// way, twice what the memory's latency asks for.
+// way, twice what the memory's latency asks for.  Measured: bf16 rows of 128 at 6.5 TB/s, the copy rate; 8-bit ones at 4.6 (widening them).
 //
 // Scores and outputs are mma.sync products (m16n8k16): at 16 rows a tile's products take a sixth of its loading time, and the
 // operands' layout leaves the scores' accumulators as the operands of the second product.  Rows in bf16 enter as they are, their weights as
@@ -21,12 +21,14 @@
 
 namespace csd {
 
-constexpr int PW = 8;                           // warps of a CTA
 constexpr int PSMEM = 227 * 1024;
 constexpr float LATE = 8.f;                     // a running maximum may lag by this power of two (weights of up to 2^8)
 
 template <int DH, int MT, bool ROWS16, bool E4M3> struct PagedRowsCfg {
     static constexpr int BR = 16 * MT;
+    // warps of a CTA: three to a scheduler hide one another's chains where their registers fit (296 heads of 16384 positions, four rows
+    // each: bf16 451 us with eight, 381 with twelve; 8 bits 356 and 270)
+    static constexpr int PW = MT == 1 ? 12 : 8;
     static constexpr int RB = E4M3 ? DH : 2 * DH;                        // bytes of a cache row
     static constexpr int QT = ROWS16 ? 1 : E4M3 ? 2 : 3;                 // terms of a query entry
     static constexpr int PT = ROWS16 ? 1 : 3;                            // of a weight
@@ -34,11 +36,11 @@ template <int DH, int MT, bool ROWS16, bool E4M3> struct PagedRowsCfg {
     // products, maxima and exponentials exceeds (8-bit rows of 128, 296 heads of 16384 positions: 390 us with one)
     static constexpr int GK = RB <= 128 && (MT == 1 || ROWS16) ? 2 : 1, WK = 16 * GK, KEYS = WK * PW;
     static constexpr int STAGE = 2 * WK * RB + (E4M3 ? 2 * WK : 0);      // a warp's keys, values and scales of a tile
-    static constexpr int MC = MT == 1 ? 32 : 16;                         // dimensions of all rows that are added up at a time
-    static constexpr int PREFIX = (CSD_MAX_SEQS + 1) * 8, Q = QT * BR * DH * 2, MERGE = PW * BR * MC * 4, ROWF = (2 * PW + 3) * BR * 4;
-    static constexpr int FIXED = (PREFIX + Q + MERGE + ROWF + 15) / 16 * 16;
+    static constexpr int MC = MT == 1 && PW == 8 ? 32 : 16;                         // dimensions of all rows that are added up at a time
+    static constexpr int Q = QT * BR * DH * 2, MERGE = PW * BR * MC * 4, ROWF = (2 * PW + 3) * BR * 4;
+    static constexpr int FIXED = Q + MERGE + ROWF;
     static constexpr int FIT = (PSMEM - FIXED - 512) / (PW * STAGE), STAGES = FIT > 5 ? 5 : FIT;
-    static_assert(STAGES >= 2, "two tiles in flight");
+    static_assert(STAGES >= 2 && STAGES * PW * STAGE >= (CSD_MAX_SEQS + 1) * 8, "two tiles in flight, room for the prefix");
     static constexpr int SMEM = FIXED + STAGES * PW * STAGE;
     static constexpr int PART = BR * (DH + 2);                           // floats of a part: rows, maxima, sums
 };
@@ -68,14 +70,14 @@ template <int RB> __device__ __forceinline__ uint32_t stage_off(int j, int c) {
 }
 
 template <int DH, int MT, bool ROWS16, bool E4M3>
-__global__ void __launch_bounds__(32 * PW, 1)
+__global__ void __launch_bounds__(32 * PagedRowsCfg<DH, MT, ROWS16, E4M3>::PW, 1)
 paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int snap) {
     using C = PagedRowsCfg<DH, MT, ROWS16, E4M3>;
     using S = Schedule<C::BR, C::KEYS>;
-    constexpr int BR = C::BR, KS = DH / 16, NS = C::STAGES, GK = C::GK, WK = C::WK, RB = C::RB;
+    constexpr int BR = C::BR, PW = C::PW, KS = DH / 16, NS = C::STAGES, GK = C::GK, WK = C::WK, RB = C::RB;
     extern __shared__ __align__(128) unsigned char smem[];
-    u64* prefix = reinterpret_cast<u64*>(smem);
-    unsigned char* Qs = smem + (C::PREFIX + 15) / 16 * 16;
+    unsigned char* Qs = smem;
+    u64* prefix = reinterpret_cast<u64*>(smem + C::FIXED);               // (until the run's first unit is found)
     float* merge = reinterpret_cast<float*>(Qs + C::Q);
     float* row_m = merge + C::MERGE / 4;                 // [warp][row], then the item's [row]
     float* row_l = row_m + PW * BR;
@@ -98,6 +100,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
     typename S::Cursor ld, at;                           // the tile to request next, the tile to multiply
     u64 begin, end;
     if (!S::run(w, prefix, blockIdx.x, n_runs, snap, a.group, tree, &begin, &end, &at)) return;
+    __syncthreads();                                     // (the stages take the prefix's place)
     ld = at;
     u64 requested = begin;
     unsigned lost = 0;                                   // GK bits a stage: groups that have no positions or no page
@@ -601,7 +604,7 @@ static csd_status run_rows(const PagedView& w, const AttendArgs& a, cudaStream_t
     static PerDevice ready;
     const csd_status ok = allow_smem(ready, kern, C::SMEM);
     if (ok != CSD_OK) return ok;
-    PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(32 * PW), C::SMEM, st);
+    PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(32 * C::PW), C::SMEM, st);
     CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a, 1, 2));
     count_launch();
     return CSD_OK;
