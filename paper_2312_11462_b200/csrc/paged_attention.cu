@@ -9,7 +9,7 @@ static csd_status check_attend(const csd_kv_pool* pool, const csd_paged_batch* b
     if (ok != CSD_OK) return ok;
     if (n_heads < 1 || n_heads % pool->n_kv_heads || n_heads / pool->n_kv_heads > 64) return CSD_ERR_SHAPE;
     if (row_type != CSD_F32 && row_type != CSD_BF16) return CSD_ERR_INVALID_ARG;
-    if ((long long)pool->n_kv_heads * (w->capacity / 128 + 1) >= 1ll << 31) return CSD_ERR_CAPACITY;       // key tiles of a row block
+    if ((long long)pool->n_kv_heads * (w->capacity / 128 + 8) >= 1ll << 31) return CSD_ERR_CAPACITY;       // units of a row block (paged_schedule.cuh)
     return (long long)batch->max_rows * (n_heads / pool->n_kv_heads) < 1 << 30 ? CSD_OK : CSD_ERR_CAPACITY;
 }
 

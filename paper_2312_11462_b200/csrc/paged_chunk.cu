@@ -123,7 +123,7 @@ __device__ __forceinline__ bool wait_long(uint64_t* bar, uint32_t parity, volati
     return false;
 }
 
-typedef Schedule<CH_ROWS, CH_KEYS> ChunkSchedule;
+typedef Schedule<CH_ROWS, CH_KEYS, 2> ChunkSchedule;
 
 // What a run has of an item, and the halves' own ends.
 struct ChunkPiece {
@@ -131,10 +131,9 @@ struct ChunkPiece {
     int end[2], see[2];                                          // a half's last tile + 1, positions that all its rows see
     bool whole;
     __device__ __forceinline__ ChunkPiece(const PagedView& w, const ChunkSchedule::Cursor& at, u64 run_end, int group) {
-        const u64 item_end = at.item_first + at.tiles;
         first = at.tile;
-        stop = (int)((item_end < run_end ? item_end : run_end) - at.item_first);
-        whole = first == 0 && item_end <= run_end;
+        stop = at.tiles_before(run_end);
+        whole = first == 0 && at.item_end() <= run_end;
         p0 = at.rb * CH_ROWS;
         nrows = min(CH_ROWS, at.q.rows * group - p0);
 #pragma unroll
@@ -197,7 +196,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 
     u64 unit = begin;
     auto advance = [&](const ChunkPiece& p) {
-        unit = at.item_first + p.stop;
+        unit = at.unit_of(p.stop);
         if (unit < end) { at.tile = p.stop - 1; at.next(w, group, false); }
     };
 

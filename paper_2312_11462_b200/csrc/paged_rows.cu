@@ -73,7 +73,7 @@ template <int DH, int MT, bool ROWS16, bool E4M3>
 __global__ void __launch_bounds__(32 * PagedRowsCfg<DH, MT, ROWS16, E4M3>::PW, 1)
 paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int snap) {
     using C = PagedRowsCfg<DH, MT, ROWS16, E4M3>;
-    using S = Schedule<C::BR, C::KEYS>;
+    using S = Schedule<C::BR, C::KEYS, 2>;
     constexpr int BR = C::BR, PW = C::PW, KS = DH / 16, NS = C::STAGES, GK = C::GK, WK = C::WK, RB = C::RB;
     extern __shared__ __align__(128) unsigned char smem[];
     unsigned char* Qs = smem;
@@ -102,7 +102,6 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
     if (!S::run(w, prefix, blockIdx.x, n_runs, snap, a.group, tree, &begin, &end, &at)) return;
     __syncthreads();                                     // (the stages take the prefix's place)
     ld = at;
-    u64 requested = begin;
     unsigned lost = 0;                                   // GK bits a stage: groups that have no positions or no page
     // Pages of this warp's groups, a lane a group: of tiles paged .. of the item at ld (what is found is checked when it is used)
     int pages = -1, paged = 0;
@@ -114,7 +113,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
     look_up();
     // Requests the positions of the tile at ld into a stage.
     auto request = [&](int slot) {
-        if (requested < end) {
+        if (ld.unit_of(ld.tile) < end) {
             const uint32_t dst = st0 + slot * C::STAGE;
             lost &= ~(((1u << GK) - 1) << (slot * GK));
 #pragma unroll
@@ -136,8 +135,9 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                 }
                 if (E4M3 && lane < 2) cp_async16(dst + 2 * WK * RB + 16 * q + WK * lane, (lane ? w.v_exp : w.k_exp) + row, is);
             }
-            if (++requested < end) {
-                ld.next(w, a.group, tree);
+            // (behind the run's last tile the cursor stays on it, one tile too far)
+            if (ld.tile + 1 < ld.tiles || ld.item_end() < end) ld.next(w, a.group, tree); else ++ld.tile;
+            if (ld.unit_of(ld.tile) < end && ld.tile < ld.tiles) {
                 if (ld.tile == 0 || ld.tile == paged + 32 / GK) look_up();
             }
         }
@@ -150,8 +150,8 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
     u64 unit = begin;
     while (unit < end) {
         // ---- an item, or the part of it that this run has
-        const u64 item_end = at.item_first + at.tiles;
-        const int first_tile = at.tile, stop = (int)((item_end < end ? item_end : end) - at.item_first);
+        const u64 item_end = at.item_end();
+        const int first_tile = at.tile, stop = at.tiles_before(end);
         const int p0 = at.rb * BR, nrows = min(BR, at.q.rows * a.group - p0);
         __syncthreads();                                 // (the item before has left Qs and the row arrays)
         {   // the block's queries as operand rows
@@ -588,7 +588,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                 }
             }
         }
-        unit = at.item_first + stop;
+        unit = at.unit_of(stop);
         if (unit < end) {
             at.tile = stop - 1;
             at.next(w, a.group, tree);

@@ -1,6 +1,8 @@
-// How the attention over the paged cache divides its work: units are (sequence, row block, kv head, key tile), in this order, and
-// a CTA takes an equal run of them whatever the sequences' lengths are.  A run that begins or ends inside an item (all but
-// its key tile) leaves its part of the item in the workspace, and the CTA that arrives last adds the parts up, in their order.
+// How the attention over the paged cache divides its work.  An item is a (sequence, row block, kv head); it takes OVER units of time,
+// for its queries and for its rows on their way out, and one for each of its key tiles.  The items' units lie one behind the other in the
+// order of the indices, and a CTA takes an equal run of them whatever the sequences' lengths are.  (Eight sequences of 77 to 2048
+// positions, trees of 12 rows, 32 heads, with tiles alone counted: 56 us, 37 where the lengths are even.)  A run that begins or ends inside an item
+// leaves its part of the item in the workspace, and the CTA that arrives last adds the parts up, in their order.
 // A row of a row block is a (new row, query head of the group) pair: row p of the sequence's rows * group.
 #pragma once
 #include "paged.cuh"
@@ -18,7 +20,7 @@ struct AttendArgs {
     float* parts;                // [CTAs][2] parts
 };
 
-template <int BR, int KEYS> struct Schedule {
+template <int BR, int KEYS, int OVER> struct Schedule {
     // Positions that the rows of block rb see at most.  (rows * group fits 30 bits: check_attend)
     static __device__ __forceinline__ int seen(const PagedView& w, const PagedSeq& q, int rb, int group, bool tree) {
         const int last = tree ? q.rows : min(q.rows, (int)(((unsigned)(rb + 1) * BR - 1) / (unsigned)group) + 1);
@@ -40,14 +42,14 @@ template <int BR, int KEYS> struct Schedule {
             PagedSeq q = {0, 0, 0};
             if (s < w.n_seqs) q = paged_seq(w, s);
             const int nb = blocks(q, group);
-            u64 n = nb > 0 ? tiles_of(w, q, 0, group, tree) : 0u;
+            u64 n = nb > 0 ? tiles_of(w, q, 0, group, tree) + OVER : 0u;
             // sequences of several blocks, a lane a block
             for (unsigned many = __ballot_sync(0xffffffffu, nb > 1); many; many &= many - 1) {
                 const int j = __ffs(many) - 1;
                 const PagedSeq o = {0, __shfl_sync(0xffffffffu, q.rows, j), __shfl_sync(0xffffffffu, q.kv, j)};
                 const int all = __shfl_sync(0xffffffffu, nb, j);
                 u64 sum = 0;
-                for (int rb = 1 + lane; rb < all; rb += 32) sum += tiles_of(w, o, rb, group, tree);
+                for (int rb = 1 + lane; rb < all; rb += 32) sum += tiles_of(w, o, rb, group, tree) + OVER;
 #pragma unroll
                 for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
                 if (lane == j) n += sum;
@@ -79,11 +81,16 @@ template <int BR, int KEYS> struct Schedule {
         PagedSeq q;
         int s, rb, h, tile, tiles, seen;
 
+        __device__ __forceinline__ u64 unit_of(int t) const { return item_first + OVER + t; }      // of a tile
+        __device__ __forceinline__ u64 item_end() const { return unit_of(tiles); }
+        // the item's tiles in front of a run's end
+        __device__ __forceinline__ int tiles_before(u64 end) const { return item_end() <= end ? tiles : (int)(end - unit_of(0)); }
+
         __device__ __forceinline__ void block(const PagedView& w, int group, bool tree) {
             seen = Schedule::seen(w, q, rb, group, tree);
             tiles = (seen + KEYS - 1) / KEYS;
         }
-        // unit < prefix[n_seqs]; whole warps
+        // to the item of a unit < prefix[n_seqs], and the tile there (the first, in front of it); whole warps
         __device__ void seek(const PagedView& w, const u64* prefix, u64 unit, int group, bool tree) {
             const int lane = threadIdx.x & 31;
             int lo = 0, hi = w.n_seqs - 1;               // the last s with prefix[s] <= unit
@@ -98,7 +105,7 @@ template <int BR, int KEYS> struct Schedule {
             rb = 0;
             if (nb > 1)
                 for (int b0 = 0;; b0 += 32) {            // a lane a block
-                    const u64 n = b0 + lane < nb ? (u64)tiles_of(w, q, b0 + lane, group, tree) * w.heads : 0;
+                    const u64 n = b0 + lane < nb ? (u64)(tiles_of(w, q, b0 + lane, group, tree) + OVER) * w.heads : 0;
                     u64 x = n;
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
@@ -112,15 +119,14 @@ template <int BR, int KEYS> struct Schedule {
                     if (k < 32) break;
                 }
             block(w, group, tree);
-            h = (int)((unsigned)(unit - at) / (unsigned)tiles);
-            if ((unit - at) >> 32) h = (int)((unit - at) / (u64)tiles);
-            item_first = at + (u64)h * tiles;
-            tile = (int)(unit - item_first);
+            h = (int)((unsigned)(unit - at) / (unsigned)(tiles + OVER));         // (a block's units fit 32 bits: check_attend)
+            item_first = at + (u64)h * (tiles + OVER);
+            tile = max((int)(unit - item_first) - OVER, 0);
         }
-        // to the next unit; there has to be one
+        // to the next tile; there has to be one
         __device__ __forceinline__ void next(const PagedView& w, int group, bool tree) {
             if (++tile < tiles) return;
-            item_first += tiles;
+            item_first = item_end();
             tile = 0;
             if (++h < w.heads) return;
             h = 0;
@@ -132,30 +138,32 @@ template <int BR, int KEYS> struct Schedule {
         }
     };
 
-    // What CTA c of n takes: units [begin, end), with `at` at begin.  An equal share, but that a cut within `snap` tiles of an item's
-    // end moves there: a part costs its writing, its adding up and another start.  False: nothing is left for this CTA.
+    // What CTA c of n takes: units [begin, end), with `at` at its first tile.  An equal share, but that a cut in front of an item's first tile or within
+    // `snap` tiles of an item's end moves there: a part costs its writing, its adding up and another start.  False: nothing is left for this CTA.
     static __device__ bool run(const PagedView& w, const u64* prefix, int c, unsigned n, int snap, int group, bool tree, u64* begin, u64* end, Cursor* at) {
         const u64 units = prefix[w.n_seqs];
         const bool one = w.max_rows * group <= BR;       // one block a sequence: its items are alike
         auto cut = [&](int i) {
             const u64 raw = (u64)i * units / n;
             if (raw == 0 || raw >= units) return raw;
-            int tile, tiles;
+            u64 first;
+            int tiles;
             if (one) {
                 int lo = 0, hi = w.n_seqs - 1;
                 while (lo < hi) {
                     const int mid = (lo + hi + 1) >> 1;
                     if (prefix[mid] <= raw) lo = mid; else hi = mid - 1;
                 }
-                const unsigned all = (unsigned)(prefix[lo + 1] - prefix[lo]);        // (a sequence has fewer than 2^30 / KEYS tiles a head)
-                tiles = (int)(all / (unsigned)w.heads);
-                tile = (int)((unsigned)(raw - prefix[lo]) % (unsigned)tiles);
+                const unsigned each = (unsigned)(prefix[lo + 1] - prefix[lo]) / (unsigned)w.heads, in = (unsigned)(raw - prefix[lo]) % each;
+                tiles = (int)each - OVER;
+                first = raw - in;
             } else {
                 at->seek(w, prefix, raw, group, tree);
-                tile = at->tile; tiles = at->tiles;
+                first = at->item_first; tiles = at->tiles;
             }
-            if (tile <= min(snap, tiles / 2)) return raw - tile;
-            return tiles - tile <= snap ? raw - tile + tiles : raw;
+            const int tile = max((int)(raw - first) - OVER, 0);
+            if (tile <= min(snap, tiles / 2)) return first;
+            return tiles - tile <= snap ? first + OVER + tiles : raw;
         };
         *end = cut(c + 1);
         *begin = cut(c);
@@ -166,7 +174,7 @@ template <int BR, int KEYS> struct Schedule {
     // The first and the last CTA that have a part of an item.
     static __device__ __forceinline__ void parts_of(const Cursor& at, u64 units, unsigned n, int snap, int* c0, int* c1) {
         auto last = [&](u64 unit) { return (int)(((unit + 1) * n - 1) / units); };      // the last CTA whose equal share begins at or before a unit
-        const u64 front = at.item_first + min(snap, at.tiles / 2), back = at.item_first + max(at.tiles - snap - 1, 0);
+        const u64 front = at.unit_of(min(snap, at.tiles / 2)), back = at.unit_of(max(at.tiles - snap - 1, 0));
         *c0 = last(front);
         *c1 = last(front > back ? front : back);
     }
