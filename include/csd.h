@@ -346,6 +346,17 @@ csd_status csd_paged_attention(const csd_kv_pool* pool, const csd_paged_batch* b
                                int row_type, float scale, const uint64_t* tree_mask_dev, void* out_dev, int64_t ldo,
                                void* workspace_dev, size_t workspace_bytes, void* stream);
 
+/* csd_review_forward over a paged cache, for one or several sequences at once: one handle, whose own cache is not used, serves any
+ * number of them.  pools is a host array, a pool for each layer (n_heads heads of d_head 64 or 128); the batch's rows
+ * (total_rows <= max_rows) are the block's tokens, rows of a sequence at positions kv_len ..; logits_out_dev [total_rows, vocab] or
+ * NULL.  tree_mask_dev: as in csd_paged_attention; a row sits at rotary position kv_len + number of its ancestors (the rows of its mask
+ * other than itself) and in the cache at its index, as in csd_review_forward_tree.  A rotary position of max_seq or more sets the
+ * device status to CSD_ERR_CAPACITY.  Rows that belong to no sequence have no meaningful logits.  arch 0 only.  The workspace
+ * is that of csd_paged_attention for fp32 rows.  The structs are read before the call returns. */
+csd_status csd_review_forward_paged(csd_model* m, const csd_kv_pool* pools, const csd_paged_batch* batch, const int32_t* block_tokens_dev,
+                                    const uint64_t* tree_mask_dev, float* logits_out_dev, void* workspace_dev, size_t workspace_bytes,
+                                    void* stream);
+
 /* ---------------------------------------------------------------------------------------------
  * Max-Gram statistical drafter (Section 3.3, Appendix A): the longest suffix of the sequence
  * (at most max_order tokens) that occurs in the haystack followed by at least one haystack

@@ -109,6 +109,7 @@ lib.csd_paged_read.argtypes = [_vp, _vp, _vp, _vp, _i64, _i, _vp]
 lib.csd_paged_attention_workspace_bytes.restype = _sz
 lib.csd_paged_attention_workspace_bytes.argtypes = [_vp, _vp, _i, _i]
 lib.csd_paged_attention.argtypes = [_vp, _vp, _vp, _i64, _i, _i, _f, _vp, _vp, _i64, _vp, _sz, _vp]
+lib.csd_review_forward_paged.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 lib.csd_mag_workspace_bytes.restype = _sz
 lib.csd_mag_workspace_bytes.argtypes = [_i, _i, _i]
 lib.csd_mag_create.argtypes = [_vp, _i, _i, _vp, _i, _i, _vp, _sz, _vp, _vp]
@@ -202,6 +203,26 @@ class Model:
         _check("csd_review_forward_tree",
                lib.csd_review_forward_tree(self.h, _ptr(block_tokens), par.ctypes.data_as(_vp), m, kv_len, _ptr(out), _stream()))
         return out
+
+    def csd_review_forward_paged(self, block_tokens: torch.Tensor, pools: Sequence["KvPool"], batch: "PagedBatch",
+                                 tree_mask: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                 logits_out: Optional[torch.Tensor] = None, append_only: bool = False):
+        """Logits [total_rows, vocab] of the batch's rows over a paged cache, a pool for each layer; the handle's own cache is not
+        used.  A workspace is zero before its first call (csd_paged_attention_workspace of a layer's pool, float32)."""
+        assert block_tokens.dtype == torch.int32 and block_tokens.is_cuda and block_tokens.is_contiguous() and block_tokens.numel() == batch.total_rows
+        assert len(pools) == self.shape.n_layers
+        if workspace is None:
+            workspace = csd_paged_attention_workspace(pools[0], batch, self.shape.n_heads, torch.float32)
+        if append_only:
+            logits_out = None
+        elif logits_out is None:
+            logits_out = torch.empty(batch.total_rows, self.shape.vocab, dtype=torch.float32, device=block_tokens.device)
+        if tree_mask is not None:
+            assert tree_mask.dtype == torch.int64 and tree_mask.is_contiguous() and tree_mask.numel() == batch.total_rows
+        structs = (KvPoolStruct * len(pools))(*[p.c for p in pools])
+        _call("csd_review_forward_paged", lib.csd_review_forward_paged, block_tokens.get_device(), self.h, C.addressof(structs), batch.ref,
+              block_tokens.data_ptr(), _ptr(tree_mask), _ptr(logits_out), workspace.data_ptr(), workspace.numel())
+        return logits_out
 
     def csd_prefill(self, tokens: torch.Tensor, kv_len: int) -> None:
         """Appends the tokens to the cache (wide blocks where the model allows them); no logits."""

@@ -1,6 +1,7 @@
 // Model handle and the review forward: one pass of a transformer over a block of m <= 17 rows
 // that streams the bf16 weights once, reads the bf16 K/V cache and appends the block to it.
 #include "model.cuh"
+#include "paged_attention.cuh"
 #include <math.h>
 #include <new>
 #include <stdlib.h>
@@ -806,9 +807,11 @@ extern "C" csd_status csd_prefill(csd_model* M, const int32_t* tokens_dev, int n
 // A block may hold the rows of several sequences (batched review): the contractions run once over
 // all rows, the attention per sequence over that sequence's own cache.
 struct Segment { csd_model* S; int row0, rows, kv_len; };
+// The block's rows lie in a paged cache instead: a pool a layer, the batch, masks of a tree or null, the attention's workspace.
+struct PagedBlock { const csd_kv_pool* pools; const csd_paged_batch* batch; const uint64_t* tree; void* ws; size_t ws_bytes; };
 static csd_status review_forward_impl(csd_model* M, const int32_t* block_tokens_dev, int m, int kv_len,
                                       float* logits_out_dev, void* stream, const unsigned* tree_mask, const int* tree_depth,
-                                      const Segment* segs = nullptr, int nseg = 0);
+                                      const Segment* segs = nullptr, int nseg = 0, const PagedBlock* paged = nullptr);
 
 extern "C" csd_status csd_review_forward(csd_model* M, const int32_t* block_tokens_dev, int m, int kv_len,
                                          float* logits_out_dev, void* stream) {
@@ -857,15 +860,35 @@ extern "C" csd_status csd_review_forward_tree(csd_model* M, const int32_t* block
     return review_forward_impl(M, block_tokens_dev, m, kv_len, logits_out_dev, stream, mask, depth);
 }
 
+extern "C" csd_status csd_review_forward_paged(csd_model* M, const csd_kv_pool* pools, const csd_paged_batch* batch, const int32_t* block_tokens_dev,
+                                               const uint64_t* tree_mask_dev, float* logits_out_dev, void* workspace_dev,
+                                               size_t workspace_bytes, void* stream) {
+    if (!M || !pools || !batch) return CSD_ERR_INVALID_ARG;
+    const csd_model_config& c = M->cfg;
+    if (c.arch != 0) return CSD_ERR_UNSUPPORTED;               // (the paged attention knows no bias)
+    PagedView w;
+    for (int l = 0; l < c.n_layers; ++l) {
+        CSD_TRY(paged_view(pools + l, batch, &w));
+        if (pools[l].n_kv_heads != c.n_heads || pools[l].d_head != c.d_head) return CSD_ERR_SHAPE;
+        const size_t need = csd_paged_attention_workspace_bytes(pools + l, batch, c.n_heads, CSD_F32);
+        if (need == 0 || workspace_bytes < need) return CSD_ERR_CAPACITY;
+    }
+    if (batch->total_rows > c.max_rows || (tree_mask_dev && batch->max_rows > 64)) return CSD_ERR_INVALID_ARG;
+    if (batch->total_rows == 0) return CSD_OK;
+    if (!workspace_dev || (((uintptr_t)workspace_dev) & 255)) return CSD_ERR_INVALID_ARG;
+    const PagedBlock paged{pools, batch, tree_mask_dev, workspace_dev, workspace_bytes};
+    return review_forward_impl(M, block_tokens_dev, batch->total_rows, 0, logits_out_dev, stream, nullptr, nullptr, nullptr, 0, &paged);
+}
+
 static csd_status review_forward_impl(csd_model* M, const int32_t* block_tokens_dev, int m, int kv_len,
                                       float* logits_out_dev, void* stream, const unsigned* tree_mask, const int* tree_depth,
-                                      const Segment* segs, int nseg) {
+                                      const Segment* segs, int nseg, const PagedBlock* paged) {
     if (!M || !block_tokens_dev) return CSD_ERR_INVALID_ARG;
     const Segment whole{M, 0, m, kv_len};
     if (!segs) { segs = &whole; nseg = 1; }
     const csd_model_config& c = M->cfg;
     if (m < 1 || m > c.max_rows || kv_len < 0) return CSD_ERR_INVALID_ARG;
-    for (int g = 0; g < nseg; ++g)                 // (of a batch, each block behind its own sequence's cache)
+    for (int g = 0; g < nseg && !paged; ++g)       // (of a batch, each block behind its own sequence's cache)
         if (segs[g].kv_len + segs[g].rows > c.max_seq) return CSD_ERR_CAPACITY;
     if (c.arch == 1 && M->enc_len < 1) return CSD_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)stream;
@@ -903,7 +926,16 @@ static csd_status review_forward_impl(csd_model* M, const int32_t* block_tokens_
             CSD_TRY(project_qkv(M, y, M->x, m, M->qkv, st, &qo));
         }
         AttnArgs blocks[CSD_MAX_ROWS];
-        for (int g = 0; g < nseg; ++g) {
+        if (paged) {
+            // keys are turned as they are written, queries as they are read; the rows leave in fp32
+            const RopeView rope{M->rope_c, M->rope_s, c.max_seq};
+            ProfScope ps(M, 1, st);
+            CSD_TRY(paged_append_turned(paged->pools + l, paged->batch, M->qkv + di, M->qkv + 2 * di, 3 * di, rope,
+                                        (const unsigned long long*)paged->tree, stream));
+            CSD_TRY(paged_attention_turned(paged->pools + l, paged->batch, M->qkv, 3 * di, H, 1.f / sqrtf((float)Dh), rope, paged->tree, M->attn, di,
+                                           paged->ws, paged->ws_bytes, stream));
+        }
+        for (int g = 0; g < nseg && !paged; ++g) {
             const Segment& sg = segs[g];
             AttnArgs& a = blocks[g];
             a.q = M->qkv + (size_t)sg.row0 * 3 * di; a.ldq = 3 * di; a.m = sg.rows;
@@ -919,10 +951,10 @@ static csd_status review_forward_impl(csd_model* M, const int32_t* block_tokens_
             a.tree_mask = tree_mask; a.tree_depth = tree_depth;
             if (tc_o) { a.out_xs = M->xs_attn; a.out_xs_ld = di; a.out_xs_rows = m; a.out_xs_row0 = sg.row0; }
         }
-        CSD_TRY(attention(M, blocks, nseg, st));
+        if (!paged) CSD_TRY(attention(M, blocks, nseg, st));
         // output projection into the residual rows; hands them on to the norm that follows
         LinOpt oo;
-        if (tc_o) oo.xs_in = M->xs_attn;
+        if (tc_o && !paged) oo.xs_in = M->xs_attn;
         const __nv_bfloat16* after_o = c.arch == 1 ? y.norm_x : y.norm2;
         x_ready = tc_o && (c.arch == 1 ? linear_uses_tensor_cores(m, di, d, false) : linear_uses_tensor_cores(m, ff, d, true));
         if (x_ready) { oo.out_xs = M->xs_x; oo.out_ld = d; oo.out_gain = after_o; oo.out_ssq = M->ssq_x; }

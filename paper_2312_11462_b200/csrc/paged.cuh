@@ -47,6 +47,9 @@ inline bool paged_rows_ok(const void* p, int64_t ld, int64_t width) {
     return p && ld >= width && (ld & 7) == 0 && (((uintptr_t)p) & 15) == 0;
 }
 
+// Rotary tables [positions][d_head / 2] of a model whose rows still have to be turned (null: they come turned).
+struct RopeView { const float* cos; const float* sin; int positions; };
+
 // ---- device side
 struct PagedSeq { int start, rows, kv; };               // first row, rows, positions before them
 
@@ -59,6 +62,21 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedView& w, int s) {
     if (lo != a || hi != b || q.rows != hi - lo || kv < 0) set_status(w.status, CSD_ERR_INVALID_ARG);
     if (q.rows > 0 && (long long)max(kv, 0) + q.rows > w.capacity) set_status(w.status, CSD_ERR_CAPACITY);
     return q;
+}
+
+// Rotary position of row i of a chunk: behind its ancestors, which are the rows of its mask other than itself; without masks all rows before it.
+__device__ __forceinline__ int rope_position(const PagedView& w, const RopeView& r, int kv, int i, const unsigned long long* mask) {
+    const int pos = kv + (mask ? __popcll(*mask & ~(1ull << (i & 63))) : i);
+    if (pos >= r.positions) set_status(w.status, CSD_ERR_CAPACITY);
+    return min(pos, r.positions - 1);
+}
+// Turns 8 neighbouring dimensions x, of column col of a row, with those half a row away.
+__device__ __forceinline__ void rope8(const RopeView& r, int pos, int half, int col, float* x, const float* other) {
+    const bool upper = col >= half;
+    const float* c = r.cos + (size_t)pos * half + (col - (upper ? half : 0));
+    const float* s = r.sin + (size_t)pos * half + (col - (upper ? half : 0));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = upper ? other[j] * s[j] + x[j] * c[j] : x[j] * c[j] - other[j] * s[j];
 }
 
 // Page of position t of sequence s; -1 where there is none.

@@ -25,13 +25,13 @@ extern "C" size_t csd_paged_attention_workspace_bytes(const csd_kv_pool* pool, c
     if (check_attend(pool, batch, n_heads, row_type, &w) != CSD_OK) return 0;
     // (the call's scale and masks are not known here: room for either kernel)
     const int packed = packed_rows(batch, pool, n_heads);
-    const size_t rows = paged_rows_workspace(pool->d_head, packed, row_type, w.k_exp != nullptr), chunk = paged_chunk_workspace(pool->d_head);
+    const size_t rows = paged_rows_workspace(pool->d_head), chunk = paged_chunk_workspace(pool->d_head);
     return takes_chunks(packed, row_type) && chunk > rows ? chunk : rows;
 }
 
-extern "C" csd_status csd_paged_attention(const csd_kv_pool* pool, const csd_paged_batch* batch, const void* q_dev, int64_t ldq, int n_heads,
-                                          int row_type, float scale, const uint64_t* tree_mask_dev, void* out_dev, int64_t ldo,
-                                          void* workspace_dev, size_t workspace_bytes, void* stream) {
+static csd_status attend(const csd_kv_pool* pool, const csd_paged_batch* batch, const void* q_dev, int64_t ldq, int n_heads, int row_type, float scale,
+                         const RopeView& rope, const uint64_t* tree_mask_dev, void* out_dev, int64_t ldo, void* workspace_dev, size_t workspace_bytes,
+                         void* stream) {
     PagedView w;
     const csd_status ok = check_attend(pool, batch, n_heads, row_type, &w);
     if (ok != CSD_OK) return ok;
@@ -43,9 +43,21 @@ extern "C" csd_status csd_paged_attention(const csd_kv_pool* pool, const csd_pag
     if (workspace_bytes < csd_paged_attention_workspace_bytes(pool, batch, n_heads, row_type)) return CSD_ERR_CAPACITY;
     w.status = status_word_device();
     if (!w.status) return CSD_ERR_CUDA;
-    AttendArgs a{q_dev, out_dev, (const u64*)tree_mask_dev, ldq, ldo, n_heads / pool->n_kv_heads, scale, nullptr, nullptr};
+    AttendArgs a{q_dev, out_dev, (const u64*)tree_mask_dev, ldq, ldo, n_heads / pool->n_kv_heads, scale, rope, nullptr, nullptr};
     const int packed = packed_rows(batch, pool, n_heads);
     if (takes_chunks(packed, row_type) && !tree_mask_dev && scale > 0.f)
         return launch_paged_chunk(w, a, pool->d_head, workspace_dev, (cudaStream_t)stream);
     return launch_paged_rows(w, a, pool->d_head, packed, row_type, workspace_dev, (cudaStream_t)stream);
+}
+
+csd_status csd::paged_attention_turned(const csd_kv_pool* pool, const csd_paged_batch* batch, const float* q, int64_t ldq, int n_heads, float scale,
+                                       const RopeView& rope, const uint64_t* tree, float* out, int64_t ldo, void* workspace, size_t workspace_bytes,
+                                       void* stream) {
+    return attend(pool, batch, q, ldq, n_heads, CSD_F32, scale, rope, tree, out, ldo, workspace, workspace_bytes, stream);
+}
+
+extern "C" csd_status csd_paged_attention(const csd_kv_pool* pool, const csd_paged_batch* batch, const void* q_dev, int64_t ldq, int n_heads,
+                                          int row_type, float scale, const uint64_t* tree_mask_dev, void* out_dev, int64_t ldo,
+                                          void* workspace_dev, size_t workspace_bytes, void* stream) {
+    return attend(pool, batch, q_dev, ldq, n_heads, row_type, scale, RopeView{}, tree_mask_dev, out_dev, ldo, workspace_dev, workspace_bytes, stream);
 }

@@ -6,16 +6,19 @@
 //
 // A thread holds 8 neighbouring elements of one row, d_head / 8 threads a row, K and V of a head side by side; a warp belongs to
 // one position and looks it up once.  What bounds both directions is the row traffic.
-#include "paged.cuh"
+#include "paged_attention.cuh"
 #include "tc_common.cuh"
 #include <cuda_fp8.h>
 
 namespace csd {
 
-struct RowsView { const void* k; const void* v; long long ld; };
+struct RowsView {
+    const void* k; const void* v; long long ld;
+    RopeView rope; const unsigned long long* tree;       // (append alone, fp32 rows: the model's keys are turned on their way)
+};
 
 // Sequence that row r of the batch belongs to, its lengths, and the row's position; false: to none.  Whole warps.
-__device__ __forceinline__ bool find_row(const PagedView& w, int r, int* seq, int* pos) {
+__device__ __forceinline__ bool find_row(const PagedView& w, int r, int* seq, int* pos, int* row = nullptr) {
     const int lane = threadIdx.x & 31;
     int s = 0;
     for (int b = 0; b < w.n_seqs; b += 32) {
@@ -27,6 +30,7 @@ __device__ __forceinline__ bool find_row(const PagedView& w, int r, int* seq, in
     if (s >= w.n_seqs) return false;
     const PagedSeq q = paged_seq(w, s);
     *seq = s; *pos = q.kv + r - q.start;
+    if (row) *row = r - q.start;
     return r >= q.start && r - q.start < q.rows;
 }
 
@@ -73,7 +77,7 @@ paged_append_kernel(const PagedView w, const RowsView src, int split) {
     const int gw = (int)(blockIdx.x * 8 + (threadIdx.x >> 5)), r = gw / split, lane = threadIdx.x & 31;
     const int units = 2 * w.heads * (DH / 8), step = 32 * split;
     if (r >= w.total_rows) return;
-    int page = -1, pos = 0;
+    int page = -1, pos = 0, turn = 0;
     bool looked = false;
     for (int u0 = gw % split * 32; u0 < units; u0 += BATCH * step) {
         float x[BATCH][8] = {};
@@ -86,8 +90,9 @@ paged_append_kernel(const PagedView w, const RowsView src, int split) {
             }
         }
         if (!looked) {                                               // (the first loads are under way)
-            int seq;
-            if (!find_row(w, r, &seq, &pos)) return;
+            int seq, i;
+            if (!find_row(w, r, &seq, &pos, &i)) return;
+            if (!ROWS16 && src.rope.cos) turn = rope_position(w, src.rope, pos - i, i, src.tree ? src.tree + r : nullptr);
             page = paged_page(w, seq, pos);
             if (page < 0) return;
             looked = true;
@@ -98,6 +103,12 @@ paged_append_kernel(const PagedView w, const RowsView src, int split) {
             const bool live = p.head < w.heads;
             const size_t row = paged_row(w, page, live ? p.head : 0, pos);
             unsigned char* pool = const_cast<unsigned char*>(p.which ? w.v : w.k);
+            if (!ROWS16 && src.rope.cos) {                           // (the dimensions half a row away are DH / 16 lanes on)
+                float other[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) other[i] = __shfl_xor_sync(0xffffffffu, x[b][i], DH / 16);
+                if (live && !p.which) rope8(src.rope, turn, DH / 2, p.col, x[b], other);
+            }
             if constexpr (!E4M3) {
                 if (live) *reinterpret_cast<uint4*>(pool + (row * DH + p.col) * 2) = pack8_bf16(x[b]);
             } else {
@@ -215,7 +226,7 @@ template <int DH, bool R, bool E> struct ReadPick { static constexpr auto kernel
 
 template <template <int, bool, bool> class Pick>
 static csd_status run_cache(const csd_kv_pool* pool, const csd_paged_batch* batch, const void* k, const void* v, int64_t ld,
-                            int row_type, void* stream) {
+                            int row_type, const RopeView& rope, const unsigned long long* tree, void* stream) {
     PagedView w;
     const csd_status ok = paged_view(pool, batch, &w);
     if (ok != CSD_OK) return ok;
@@ -225,7 +236,12 @@ static csd_status run_cache(const csd_kv_pool* pool, const csd_paged_batch* batc
     if (!paged_rows_ok(k, ld, width) || !paged_rows_ok(v, ld, width)) return CSD_ERR_INVALID_ARG;
     w.status = status_word_device();
     if (!w.status) return CSD_ERR_CUDA;
-    return launch_cache<Pick>(w, RowsView{k, v, ld}, pool->d_head, row_type == CSD_BF16, (cudaStream_t)stream);
+    return launch_cache<Pick>(w, RowsView{k, v, ld, rope, tree}, pool->d_head, row_type == CSD_BF16, (cudaStream_t)stream);
+}
+
+csd_status paged_append_turned(const csd_kv_pool* pool, const csd_paged_batch* batch, const float* k, const float* v, int64_t ld, const RopeView& rope,
+                               const unsigned long long* tree, void* stream) {
+    return run_cache<AppendPick>(pool, batch, k, v, ld, CSD_F32, rope, tree, stream);
 }
 
 }  // namespace csd
@@ -234,10 +250,10 @@ using namespace csd;
 
 extern "C" csd_status csd_paged_append(const csd_kv_pool* pool, const csd_paged_batch* batch, const void* k_dev, const void* v_dev,
                                        int64_t ld, int row_type, void* stream) {
-    return run_cache<AppendPick>(pool, batch, k_dev, v_dev, ld, row_type, stream);
+    return run_cache<AppendPick>(pool, batch, k_dev, v_dev, ld, row_type, RopeView{}, nullptr, stream);
 }
 
 extern "C" csd_status csd_paged_read(const csd_kv_pool* pool, const csd_paged_batch* batch, void* k_dev, void* v_dev, int64_t ld,
                                      int row_type, void* stream) {
-    return run_cache<ReadPick>(pool, batch, k_dev, v_dev, ld, row_type, stream);
+    return run_cache<ReadPick>(pool, batch, k_dev, v_dev, ld, row_type, RopeView{}, nullptr, stream);
 }

@@ -148,7 +148,7 @@ struct ChunkPiece {
 
 template <int DH, bool E4M3>
 __global__ void __launch_bounds__(CH_THREADS, 1)
-paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PagedView w, const AttendArgs a, int least_units, int snap) {
+paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PagedView w, const AttendArgs a) {
     using C = ChunkCfg<DH, E4M3>;
     extern __shared__ unsigned char smem_dyn[];
     __shared__ ChunkBars bars;
@@ -161,9 +161,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 
     pdl_wait();
     ChunkSchedule::count<CH_THREADS>(w, group, false, prefix);
-    const u64 units = prefix[w.n_seqs], most = units / (unsigned)least_units;
-    const unsigned n_runs = most < 1 ? 1u : most < gridDim.x ? (unsigned)most : gridDim.x;
-    if (blockIdx.x >= n_runs || units == 0) return;
+    const u64 units = prefix[w.n_seqs];
+    const unsigned n_runs = units < gridDim.x ? (unsigned)units : gridDim.x;
+    if (blockIdx.x >= n_runs) return;
+    const int snap = ChunkSchedule::snap_of(units, n_runs, 3);
     u64 begin, end;
     ChunkSchedule::Cursor at;
     if (!ChunkSchedule::run(w, prefix, blockIdx.x, n_runs, snap, group, false, &begin, &end, &at)) return;
@@ -707,7 +708,7 @@ template <int DH, bool E4M3> static csd_status run_chunk(const PagedView& w, con
         if (!encode_map_2d(w.k, rows, DH, 1 << w.page_shift, &tk) || !encode_map_2d(w.v, rows, DH, 1 << w.page_shift, &tv)) return CSD_ERR_UNSUPPORTED;
     }
     PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(CH_THREADS), C::SMEM, st);
-    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, tk, tv, w, a, 1, 2));
+    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, tk, tv, w, a));
     count_launch();
     return CSD_OK;
 }

@@ -24,6 +24,8 @@ namespace csd {
 constexpr int PSMEM = 227 * 1024;
 constexpr float LATE = 8.f;                     // a running maximum may lag by this power of two (weights of up to 2^8)
 
+constexpr int most_dims(int rows, int dims, int bytes) { return rows * dims * 4 <= bytes ? dims : most_dims(rows, dims / 2, bytes); }
+
 template <int DH, int MT, bool ROWS16, bool E4M3> struct PagedRowsCfg {
     static constexpr int BR = 16 * MT;
     // warps of a CTA: three to a scheduler hide one another's chains where their registers fit (296 heads of 16384 positions, four rows
@@ -36,13 +38,13 @@ template <int DH, int MT, bool ROWS16, bool E4M3> struct PagedRowsCfg {
     // products, maxima and exponentials exceeds (8-bit rows of 128, 296 heads of 16384 positions: 390 us with one)
     static constexpr int GK = RB <= 128 && (MT == 1 || ROWS16) ? 2 : 1, WK = 16 * GK, KEYS = WK * PW;
     static constexpr int STAGE = 2 * WK * RB + (E4M3 ? 2 * WK : 0);      // a warp's keys, values and scales of a tile
-    static constexpr int MC = MT == 1 && PW == 8 ? 32 : 16;                         // dimensions of all rows that are added up at a time
-    static constexpr int Q = QT * BR * DH * 2, MERGE = PW * BR * MC * 4, ROWF = (2 * PW + 3) * BR * 4;
-    static constexpr int FIXED = Q + MERGE + ROWF;
+    static constexpr int DIMS = most_dims(BR, DH, STAGE);                // dimensions of the rows that a stage has room for in fp32
+    static constexpr int Q = QT * BR * DH * 2, ROWF = (2 * PW + 3) * BR * 4;
+    static constexpr int FIXED = Q + ROWF;
     static constexpr int FIT = (PSMEM - FIXED - 512) / (PW * STAGE), STAGES = FIT > 5 ? 5 : FIT;
     static_assert(STAGES >= 2 && STAGES * PW * STAGE >= (CSD_MAX_SEQS + 1) * 8, "two tiles in flight, room for the prefix");
     static constexpr int SMEM = FIXED + STAGES * PW * STAGE;
-    static constexpr int PART = BR * (DH + 2);                           // floats of a part: rows, maxima, sums
+    static constexpr int PART = BR * (DH + 2);                           // floats of a part: rows, maxima, sums (paged_rows_workspace)
 };
 
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -71,15 +73,14 @@ template <int RB> __device__ __forceinline__ uint32_t stage_off(int j, int c) {
 
 template <int DH, int MT, bool ROWS16, bool E4M3>
 __global__ void __launch_bounds__(32 * PagedRowsCfg<DH, MT, ROWS16, E4M3>::PW, 1)
-paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int snap) {
+paged_rows_kernel(const PagedView w, const AttendArgs a) {
     using C = PagedRowsCfg<DH, MT, ROWS16, E4M3>;
-    using S = Schedule<C::BR, C::KEYS, 2>;
+    using S = Schedule<C::BR, C::KEYS, 1>;
     constexpr int BR = C::BR, PW = C::PW, KS = DH / 16, NS = C::STAGES, GK = C::GK, WK = C::WK, RB = C::RB;
     extern __shared__ __align__(128) unsigned char smem[];
     unsigned char* Qs = smem;
     u64* prefix = reinterpret_cast<u64*>(smem + C::FIXED);               // (until the run's first unit is found)
-    float* merge = reinterpret_cast<float*>(Qs + C::Q);
-    float* row_m = merge + C::MERGE / 4;                 // [warp][row], then the item's [row]
+    float* row_m = reinterpret_cast<float*>(Qs + C::Q);  // [warp][row], then the item's [row]
     float* row_l = row_m + PW * BR;
     float* row_f = row_l + PW * BR;                      // [3][row]
     __shared__ int s_last;
@@ -91,9 +92,9 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
     pdl_trigger();
     S::template count<32 * PW>(w, a.group, a.tree != nullptr, prefix);
     const u64 units = prefix[w.n_seqs];
-    const u64 most = units / (unsigned)least_units;
-    const unsigned n_runs = most < 1 ? 1u : most < gridDim.x ? (unsigned)most : gridDim.x;
-    if (blockIdx.x >= n_runs || units == 0) return;
+    const unsigned n_runs = units < gridDim.x ? (unsigned)units : gridDim.x;
+    if (blockIdx.x >= n_runs) return;
+    const int snap = S::snap_of(units, n_runs, 16);
     const bool tree = a.tree != nullptr;
     const float to_log2 = a.scale * 1.4426950408889634f;
 
@@ -168,6 +169,13 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                     } else {
                         const float4 u = *reinterpret_cast<const float4*>((const float*)a.q + src), v = *reinterpret_cast<const float4*>((const float*)a.q + src + 4);
                         x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+                        if (a.rope.cos) {
+                            const float* far = (const float*)a.q + src + (8 * c < DH / 2 ? DH / 2 : -DH / 2);
+                            const float4 y = *reinterpret_cast<const float4*>(far), z = *reinterpret_cast<const float4*>(far + 4);
+                            const float other[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
+                            const int i = p / a.group;
+                            rope8(a.rope, rope_position(w, a.rope, at.q.kv, i, a.tree ? a.tree + at.q.start + i : nullptr), DH / 2, 8 * c, x, other);
+                        }
                     }
                 }
                 if constexpr (!E4M3) {
@@ -483,15 +491,12 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
             if constexpr (ROWS16) *reinterpret_cast<uint2*>((uint16_t*)a.out + dst) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
             else *reinterpret_cast<float4*>((float*)a.out + dst) = v;
         };
-        // `dims` dimensions of the valid rows at a time through `buf` ([warp][row][dims]): all at once where they fit, and behind the
-        // run's last tile, when the stages are free
-        constexpr bool ROOM = PW * BR * DH * 4 <= NS * PW * C::STAGE;
-        float* buf = ROOM && item_end >= end ? reinterpret_cast<float*>(smem + C::FIXED) : merge;
-        int dims = DH;
-        if (buf == merge)
-            while (nrows * dims > BR * C::MC) dims >>= 1;
-#pragma unroll 1
-        for (int d0 = 0; d0 < DH; d0 += dims) {
+        // DIMS dimensions of the valid rows at a time, every warp's in its stage of the item's last tile, which the next request fills
+        constexpr int DIMS = C::DIMS;
+        unsigned char* const spare = smem + C::FIXED + (slot == 0 ? NS - 1 : slot - 1) * C::STAGE;
+        auto rows_of = [&](int j) { return reinterpret_cast<float*>(spare + j * (NS * C::STAGE)); };
+#pragma unroll
+        for (int d0 = 0; d0 < DH; d0 += DIMS) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -499,27 +504,26 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                     const int r = 16 * mt + (lane >> 2) + 8 * hr;
                     if (r >= nrows) continue;
                     const float f = row_m[warp * BR + r];
-                    float* dst = buf + (warp * nrows + r) * dims - d0;
+                    float* dst = rows_of(warp) + r * DIMS;
 #pragma unroll
-                    for (int t = 0; t < DH / 8; t += 2) {
-                        if (8 * t < d0 || 8 * t >= d0 + dims) continue;
+                    for (int t = d0 / 8; t < (d0 + DIMS) / 8; t += 2) {
                         const float a0 = o[mt][t][2 * hr] * f, a1 = o[mt][t][2 * hr + 1] * f, b0 = o[mt][t + 1][2 * hr] * f, b1 = o[mt][t + 1][2 * hr + 1] * f;
                         if constexpr (E4M3) {            // (accumulators t and t + 1: the even and the odd ones of 16)
-                            *reinterpret_cast<float4*>(dst + 8 * t + 4 * (lane & 3)) = make_float4(a0, b0, a1, b1);
+                            *reinterpret_cast<float4*>(dst + 8 * t - d0 + 4 * (lane & 3)) = make_float4(a0, b0, a1, b1);
                         } else {
-                            *reinterpret_cast<float2*>(dst + 8 * t + 2 * (lane & 3)) = make_float2(a0, a1);
-                            *reinterpret_cast<float2*>(dst + 8 * t + 8 + 2 * (lane & 3)) = make_float2(b0, b1);
+                            *reinterpret_cast<float2*>(dst + 8 * t - d0 + 2 * (lane & 3)) = make_float2(a0, a1);
+                            *reinterpret_cast<float2*>(dst + 8 * t + 8 - d0 + 2 * (lane & 3)) = make_float2(b0, b1);
                         }
                     }
                 }
             __syncthreads();
-            const int per = dims / 4;
-            for (int i = tid; i < nrows * per; i += 32 * PW) {
-                const int r = i / per, c = i % per * 4;
+            constexpr int PER = DIMS / 4;
+            for (int i = tid; i < nrows * PER; i += 32 * PW) {
+                const int r = i / PER, c = i % PER * 4;
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int j = 0; j < PW; ++j) {
-                    const float4 x = *reinterpret_cast<const float4*>(buf + (j * nrows + r) * dims + c);
+                    const float4 x = *reinterpret_cast<const float4*>(rows_of(j) + r * DIMS + c);
                     v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
                 }
                 if (whole) {
@@ -529,7 +533,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                     __stcg(reinterpret_cast<float4*>(part + r * DH + d0 + c), v);
                 }
             }
-            if (d0 + dims < DH) __syncthreads();
+            if (d0 + DIMS < DH) __syncthreads();
         }
         if (!whole) {
             // ---- the last of the item's parts to arrive adds them up, in the order of their runs
@@ -543,8 +547,9 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                 __threadfence();
                 auto of = [&](int c) { return a.parts + ((size_t)c * 2 + (c == c0 ? 1 : 0)) * C::PART; };
                 const int n_parts = c1 - c0 + 1;
-                // a warp a row, a lane a part: the row's maximum and sum; then what each part counts, in `merge`
-                constexpr int MOST = C::MERGE / 4 / BR;          // parts at a time
+                // a warp a row, a lane a part: the row's maximum and sum; then what each part counts, in a stage
+                constexpr int MOST = DIMS;                       // parts at a time
+                float* share = rows_of(0);
                 for (int r = warp; r < nrows; r += PW) {
                     float top = -INFINITY, sum = 0.f;
                     for (int c = lane; c < n_parts; c += 32) top = fmaxf(top, __ldcg(of(c0 + c) + BR * DH + r));
@@ -564,7 +569,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                     __syncthreads();
                     for (int i = tid; i < nrows * nb; i += 32 * PW) {
                         const int r = i / nb, c = i % nb;
-                        merge[r * MOST + c] = ex2(__ldcg(of(c0 + b0 + c) + BR * DH + r) - row_f[BR + r]);
+                        share[r * MOST + c] = ex2(__ldcg(of(c0 + b0 + c) + BR * DH + r) - row_f[BR + r]);
                     }
                     __syncthreads();
 #pragma unroll
@@ -573,7 +578,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a, int least_units, int sn
                         if (i >= nrows * PER) continue;
 #pragma unroll 4
                         for (int c = 0; c < nb; ++c) {
-                            const float f = merge[r * MOST + c];
+                            const float f = share[r * MOST + c];
                             const float4 x = __ldcg(reinterpret_cast<const float4*>(of(c0 + b0 + c) + r * DH + d));
                             v[e].x += f * x.x; v[e].y += f * x.y; v[e].z += f * x.z; v[e].w += f * x.w;
                         }
@@ -605,7 +610,7 @@ static csd_status run_rows(const PagedView& w, const AttendArgs& a, cudaStream_t
     const csd_status ok = allow_smem(ready, kern, C::SMEM);
     if (ok != CSD_OK) return ok;
     PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(32 * C::PW), C::SMEM, st);
-    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a, 1, 2));
+    CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, w, a));
     count_launch();
     return CSD_OK;
 }
@@ -623,17 +628,13 @@ template <class F> static auto pick_rows(int d_head, int packed_rows, int row_ty
     return packed_rows <= 16 ? four(std::integral_constant<int, 128>(), One()) : four(std::integral_constant<int, 128>(), Two());
 }
 
-struct RowsBytes {
-    template <int D, int M, bool R, bool E> size_t operator()() const { return (size_t)tc_sm_count() * 2 * PagedRowsCfg<D, M, R, E>::PART * 4; }
-};
 struct RowsRun {
     const PagedView& w; const AttendArgs& a; cudaStream_t st;
     template <int D, int M, bool R, bool E> csd_status operator()() const { return run_rows<D, M, R, E>(w, a, st); }
 };
 
-size_t paged_rows_workspace(int d_head, int packed_rows, int row_type, bool e4m3) {
-    return PAGED_TICKET_BYTES + pick_rows(d_head, packed_rows, row_type, e4m3, RowsBytes());
-}
+// (room for blocks of 32 rows, whichever a call takes: callers keep one workspace for batches of all lengths)
+size_t paged_rows_workspace(int d_head) { return PAGED_TICKET_BYTES + (size_t)tc_sm_count() * 2 * 32 * (d_head + 2) * 4; }
 
 csd_status launch_paged_rows(const PagedView& w, AttendArgs a, int d_head, int packed_rows, int row_type, void* workspace, cudaStream_t st) {
     a.tickets = (unsigned*)workspace;

@@ -16,6 +16,7 @@ struct AttendArgs {
     long long ldq, ldo;
     int group;                   // query heads a kv head
     float scale;
+    RopeView rope;               // (fp32 rows alone)
     unsigned* tickets;           // [CTAs]
     float* parts;                // [CTAs][2] parts
 };
@@ -138,6 +139,8 @@ template <int BR, int KEYS, int OVER> struct Schedule {
         }
     };
 
+    // How far a cut may move: a share of a run, two tiles at most.
+    static __device__ __forceinline__ int snap_of(u64 units, unsigned n, unsigned share) { return (int)min((u64)2, units / n / share); }
     // What CTA c of n takes: units [begin, end), with `at` at its first tile.  An equal share, but that a cut in front of an item's first tile or within
     // `snap` tiles of an item's end moves there: a part costs its writing, its adding up and another start.  False: nothing is left for this CTA.
     static __device__ bool run(const PagedView& w, const u64* prefix, int c, unsigned n, int snap, int group, bool tree, u64* begin, u64* end, Cursor* at) {

@@ -85,6 +85,22 @@ def test_attention_alone(b):
     assert b.lib.csd_paged_attention_workspace_bytes(C.byref(pool(b)), C.byref(batch(b)), 4, 0) > 0
 
 
+def test_sizes_that_pass_32_bits(b):
+    """More (row, query head) pairs or key tiles than the division of the work counts."""
+    big = batch(b, max_rows=1 << 29)
+    assert every_call(b, pool(b), big, heads=8, ldq=1024)[2] == CAPACITY
+    wide = pool(b, n_pages=1, n_kv_heads=1 << 16, page_size=16)
+    assert every_call(b, wide, batch(b, max_pages=1 << 25), ld=128 << 16, heads=1 << 16, ldq=128 << 16)[2] == CAPACITY
+
+
+def test_review_forward_paged(b):
+    """Without a model, pools or a batch: nothing is looked at."""
+    L, p, q = b.lib, C.byref(pool(b)), C.byref(batch(b))
+    assert L.csd_review_forward_paged(None, p, q, 4096, None, 4096, 1 << 18, 1 << 40, None) == INVALID
+    assert L.csd_review_forward_paged(1 << 20, None, q, 4096, None, 4096, 1 << 18, 1 << 40, None) == INVALID
+    assert L.csd_review_forward_paged(1 << 20, p, None, 4096, None, 4096, 1 << 18, 1 << 40, None) == INVALID
+
+
 def test_no_rows(b):
     """Nothing to do: no pointers are looked at."""
     assert every_call(b, pool(b), batch(b, total_rows=0), rows=None, out=None) == [0] * 3
