@@ -61,13 +61,17 @@ __device__ __forceinline__ void store8(void* p, const float* x) {
     }
 }
 
-// A position's units of eight elements: [head][K, V][column].  `split` warps share a position, each takes every split-th stretch of 32
-// units, BATCH stretches at a time with their loads in flight together.
+// A position's pieces of eight elements: [head][K, V][column], a stretch of 32 a warp and turn.  `split` warps share a position, each
+// takes every split-th stretch, BATCH of them at a time with their loads in flight together.  A lane keeps its half and column and
+// moves from head to head.
 constexpr int BATCH = 4;
-template <int DH> struct Unit {
-    int head, which, col;
-    __device__ __forceinline__ explicit Unit(int i) : head(i / (2 * (DH / 8))), which(i / (DH / 8) & 1), col(i % (DH / 8) * 8) {}
+template <int DH> struct Lane {
+    static constexpr int PER = DH / 8, HEADS = 32 / (2 * PER);           // lanes of a row, heads of a stretch
+    int which, col, head;
+    __device__ __forceinline__ Lane(int lane, int stretch) : which(lane / PER & 1), col(lane % PER * 8), head(stretch * HEADS + lane / (2 * PER)) {}
 };
+
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
 template <int DH, bool ROWS16, bool E4M3>
 __global__ void __launch_bounds__(256)
@@ -75,34 +79,35 @@ paged_append_kernel(const PagedView w, const RowsView src, int split) {
     pdl_wait();
     pdl_trigger();
     const int gw = (int)(blockIdx.x * 8 + (threadIdx.x >> 5)), r = gw / split, lane = threadIdx.x & 31;
-    const int units = 2 * w.heads * (DH / 8), step = 32 * split;
     if (r >= w.total_rows) return;
-    int page = -1, pos = 0, turn = 0;
+    const Lane<DH> p(lane, gw % split);
+    const int next = split * Lane<DH>::HEADS;                            // heads from one of the warp's stretches to its next
+    constexpr int SIZE = ROWS16 ? 2 : 4;
+    const char* from = (const char*)(p.which ? src.v : src.k) + ((size_t)r * src.ld + (size_t)p.head * DH + p.col) * SIZE;
+    unsigned char* to = nullptr;
+    uint8_t* to_exp = nullptr;
+    int turn = 0;
     bool looked = false;
-    for (int u0 = gw % split * 32; u0 < units; u0 += BATCH * step) {
+    for (int h0 = 0; h0 + gw % split * Lane<DH>::HEADS < w.heads; h0 += BATCH * next) {
         float x[BATCH][8] = {};
 #pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-            const Unit<DH> p(u0 + b * step + lane);
-            if (p.head < w.heads) {
-                const size_t at = (size_t)r * src.ld + p.head * DH + p.col;
-                load8<ROWS16>((const char*)(p.which ? src.v : src.k) + at * (ROWS16 ? 2 : 4), x[b]);
-            }
-        }
+        for (int b = 0; b < BATCH; ++b)
+            if (h0 + b * next + p.head < w.heads) load8<ROWS16>(from + (size_t)(h0 + b * next) * DH * SIZE, x[b]);
         if (!looked) {                                               // (the first loads are under way)
-            int seq, i;
+            int seq, pos, i;
             if (!find_row(w, r, &seq, &pos, &i)) return;
             if (!ROWS16 && src.rope.cos) turn = rope_position(w, src.rope, pos - i, i, src.tree ? src.tree + r : nullptr);
-            page = paged_page(w, seq, pos);
+            const int page = paged_page(w, seq, pos);
             if (page < 0) return;
+            const size_t row = paged_row(w, page, p.head, pos);      // (of a head that may not exist: not written)
+            to = const_cast<unsigned char*>(p.which ? w.v : w.k) + (row * DH + p.col) * (E4M3 ? 1 : 2);
+            if (E4M3) to_exp = const_cast<uint8_t*>(p.which ? w.v_exp : w.k_exp) + row;
             looked = true;
         }
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
-            const Unit<DH> p(u0 + b * step + lane);
-            const bool live = p.head < w.heads;
-            const size_t row = paged_row(w, page, live ? p.head : 0, pos);
-            unsigned char* pool = const_cast<unsigned char*>(p.which ? w.v : w.k);
+            const bool live = h0 + b * next + p.head < w.heads;
+            const size_t on = (size_t)(h0 + b * next) << w.page_shift;           // rows of the pool from the lane's first head
             if (!ROWS16 && src.rope.cos) {                           // (the dimensions half a row away are DH / 16 lanes on)
                 float other[8];
 #pragma unroll
@@ -110,17 +115,23 @@ paged_append_kernel(const PagedView w, const RowsView src, int split) {
                 if (live && !p.which) rope8(src.rope, turn, DH / 2, p.col, x[b], other);
             }
             if constexpr (!E4M3) {
-                if (live) *reinterpret_cast<uint4*>(pool + (row * DH + p.col) * 2) = pack8_bf16(x[b]);
+                if (live) *reinterpret_cast<uint4*>(to + on * (DH * 2)) = pack8_bf16(x[b]);
             } else {
-                unsigned bits = 0u;                                  // of the largest finite |x|, or a NaN's, which is larger
+                float top = fabsf(x[b][0]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const unsigned v = __float_as_uint(x[b][i]) & 0x7fffffffu;
-                    bits = max(bits, v == 0x7f800000u ? 0u : v);
+                for (int i = 1; i < 8; ++i) top = max_nan(top, fabsf(x[b][i]));
+#pragma unroll
+                for (int o = DH / 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+                if (__any_sync(0xffffffffu, top == INFINITY)) {      // the largest finite entry counts
+                    float finite = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) finite = fmaxf(finite, fabsf(x[b][i]) < INFINITY ? fabsf(x[b][i]) : 0.f);
+#pragma unroll
+                    for (int o = DH / 16; o > 0; o >>= 1) finite = fmaxf(finite, __shfl_xor_sync(0xffffffffu, finite, o));
+                    if (top == INFINITY) top = finite;
                 }
-#pragma unroll
-                for (int o = DH / 16; o > 0; o >>= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, o));
-                const bool nan = bits > 0x7f800000u;
+                const unsigned bits = __float_as_uint(top);
+                const bool nan = top != top;
                 const int e = nan ? 127 : max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), 27);        // exponent of the scale + 127
                 if (e == 247) {                                      // (up to 240 * 2^120: the next number, 2^128, is none in fp32)
                     const float most = __uint_as_float(0x7f700000u);
@@ -137,8 +148,8 @@ paged_append_kernel(const PagedView w, const RowsView src, int split) {
                     out[i] = (uint32_t)f | (uint32_t)g << 16;
                 }
                 if (live) {
-                    *reinterpret_cast<uint2*>(pool + row * DH + p.col) = make_uint2(out[0], out[1]);
-                    if (p.col == 0) const_cast<uint8_t*>(p.which ? w.v_exp : w.k_exp)[row] = (uint8_t)(nan ? 255 : e);
+                    *reinterpret_cast<uint2*>(to + on * DH) = make_uint2(out[0], out[1]);
+                    if (p.col == 0) to_exp[on] = (uint8_t)(nan ? 255 : e);
                 }
             }
         }
@@ -151,34 +162,37 @@ paged_read_kernel(const PagedView w, const RowsView dst, int split) {
     pdl_wait();
     pdl_trigger();
     const int gw = (int)(blockIdx.x * 8 + (threadIdx.x >> 5)), r = gw / split, lane = threadIdx.x & 31;
-    const int units = 2 * w.heads * (DH / 8), step = 32 * split;
     if (r >= w.total_rows) return;
+    const Lane<DH> p(lane, gw % split);
+    const int next = split * Lane<DH>::HEADS;
+    constexpr int SIZE = ROWS16 ? 2 : 4;
+    char* to = (char*)const_cast<void*>(p.which ? dst.v : dst.k) + ((size_t)r * dst.ld + (size_t)p.head * DH + p.col) * SIZE;
     int seq, pos;
     if (!find_row(w, r, &seq, &pos)) return;
     const int page = paged_page(w, seq, pos);
-    for (int u0 = gw % split * 32; u0 < units; u0 += BATCH * step) {
+    const size_t row = page >= 0 ? paged_row(w, page, p.head, pos) : 0;
+    const unsigned char* from = (p.which ? w.v : w.k) + (row * DH + p.col) * (E4M3 ? 1 : 2);
+    const uint8_t* from_exp = E4M3 ? (p.which ? w.v_exp : w.k_exp) + row : nullptr;
+    for (int h0 = 0; h0 + p.head < w.heads; h0 += BATCH * next) {
         uint4 raw[BATCH];
         unsigned e[BATCH];
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
-            const Unit<DH> p(u0 + b * step + lane);
             raw[b] = make_uint4(0u, 0u, 0u, 0u);
             e[b] = 127u;
-            if (p.head >= w.heads || page < 0) continue;
-            const size_t row = paged_row(w, page, p.head, pos);
-            const unsigned char* pool = p.which ? w.v : w.k;
+            if (h0 + b * next + p.head >= w.heads || page < 0) continue;
+            const size_t on = (size_t)(h0 + b * next) << w.page_shift;
             if constexpr (E4M3) {
-                const uint2 u = *reinterpret_cast<const uint2*>(pool + row * DH + p.col);
+                const uint2 u = *reinterpret_cast<const uint2*>(from + on * DH);
                 raw[b].x = u.x; raw[b].y = u.y;
-                e[b] = (p.which ? w.v_exp : w.k_exp)[row];
+                e[b] = from_exp[on];
             } else {
-                raw[b] = *reinterpret_cast<const uint4*>(pool + (row * DH + p.col) * 2);
+                raw[b] = *reinterpret_cast<const uint4*>(from + on * (DH * 2));
             }
         }
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
-            const Unit<DH> p(u0 + b * step + lane);
-            if (p.head >= w.heads) continue;
+            if (h0 + b * next + p.head >= w.heads) continue;
             float x[8];
             if constexpr (E4M3) {
                 const float scale = row_scale(e[b]);
@@ -191,8 +205,7 @@ paged_read_kernel(const PagedView w, const RowsView dst, int split) {
             } else {
                 load8<true>(&raw[b], x);
             }
-            const size_t at = (size_t)r * dst.ld + p.head * DH + p.col;
-            store8<ROWS16>((char*)const_cast<void*>(p.which ? dst.v : dst.k) + at * (ROWS16 ? 2 : 4), x);
+            store8<ROWS16>(to + (size_t)(h0 + b * next) * DH * SIZE, x);
         }
     }
 }
