@@ -18,27 +18,26 @@ struct VerifyArgs {
     int k, V;
 };
 
-constexpr int VW = 16, VMAX = 8;           // warps of a CTA, CTAs of a cluster at most
+constexpr int VW = 8, VMAX = 8;            // warps of a CTA, CTAs of a cluster at most
 constexpr int VSUMS = VW * VMAX;
 
 template <bool LAW16> __device__ __forceinline__ float law_at(const void* law, size_t i) {
     return LAW16 ? bf16_bits_to_float(((const uint16_t*)law)[i]) : ((const float*)law)[i];
 }
-// what an entry carries: positive finite numbers only
-__device__ __forceinline__ float mass_of(float x) { return x > 0.f && x < INFINITY ? x : 0.f; }
-
-// A sum of differences max(0, x - y), x and y >= 0, in a pair of fp32 numbers: x - y and each sum keep their rounding errors (the
-// differences by x >= y, the sums without a condition), so that about 46 bits of a lane's hundred entries are right.  In
-// fp64 the conversions and sums bound the pass: 256 rows of 128256 entries 120 us.
-struct Pair {
-    float hi = 0.f, lo = 0.f;
-    __device__ __forceinline__ void add(float x, float y) {
-        const float d = x > y ? x - y : 0.f, e = x > y ? (x - d) - y : 0.f;
-        const float t = hi + d, z = t - hi;
-        lo += ((hi - (t - z)) + (d - z)) + e;
-        hi = t;
-    }
-    __device__ __forceinline__ double value() const { return (double)hi + (double)lo; }
+// What is left of an entry, max(0, p - q), as a difference d in fp32 and what its rounding lost, e, so that d + e is exact: with
+// y = min(p, max(q, 0)) the subtraction of the smaller from the larger leaves an error that (p - d) - y gives exactly.  Negative
+// numbers and NaN count as 0.
+struct Left { float d, e; };
+__device__ __forceinline__ Left left_of(float p, float q) {
+    const float x = fmaxf(p, 0.f), y = fminf(x, fmaxf(q, 0.f)), d = x - y;
+    return Left{d, (x - d) - y};
+}
+// A lane's sum: the differences in fp64, their errors (2^-24 of them) in fp32.  Nine instructions an entry; with both numbers
+// converted, or in pairs of fp32, the arithmetic bounds the pass.
+struct Sum {
+    double d = 0.0; float e = 0.f;
+    __device__ __forceinline__ void add(const Left& x) { d += (double)x.d; e += x.e; }
+    __device__ __forceinline__ double value() const { return d + (double)e; }
 };
 
 __device__ __forceinline__ double warp_scan(double x, int lane) {
@@ -51,7 +50,7 @@ __device__ __forceinline__ double warp_scan(double x, int lane) {
 }
 
 template <bool LAW16>
-__global__ void __launch_bounds__(32 * VW, 2)
+__global__ void __launch_bounds__(32 * VW, 4)
 verify_kernel(const VerifyArgs a) {
     __shared__ double sums[2][VSUMS];      // of both forms of the law: the warps of the cluster in their order
     __shared__ double stretch[VW];
@@ -102,9 +101,10 @@ verify_kernel(const VerifyArgs a) {
     const size_t prow = ((size_t)row * (k + 1) + at) * a.ldp, qrow = ((size_t)row * k + at) * a.ldq;
     const int drop = at < n ? tokens[at] : -1;
     const double u = (double)uniform(k, tid == 0);
-    // this warp's piece of the vocabulary: warps of the cluster in order
-    const long long all = (long long)ctas * VW, mine = (long long)rank * VW + warp;
-    const int lo = (int)(mine * V / all), hi = (int)((mine + 1) * V / all);
+    // this warp's piece of the vocabulary: warps of the cluster in order, pieces from multiples of 8 entries on
+    const int all = ctas * VW, mine = rank * VW + warp;
+    auto piece = [&](int i) { return i >= all ? V : (int)((long long)i * V / all) & ~7; };
+    const int lo = piece(mine), hi = piece(mine + 1);
     int32_t* out = a.out + (size_t)row * (k + 1);
     if (rank == 0) {
         if (tid <= k && tid != at) out[tid] = tid < at ? tokens[tid] : -1;
@@ -112,35 +112,75 @@ verify_kernel(const VerifyArgs a) {
     }
     asm volatile("barrier.cluster.wait;" ::: "memory");
     for (int mode = at < n ? (a.q ? 0 : 1) : 2;; mode = 2) {     // p less q, p without the draft, p
-        auto entry = [&](int j) -> double {
-            const float p = mass_of(law_at<LAW16>(a.p, prow + j));
-            if (mode == 2) return (double)p;
-            if (mode == 1) return j == drop ? 0.0 : (double)p;
-            const float q = mass_of(law_at<LAW16>(a.q, qrow + j));
-            return p > q ? (double)p - (double)q : 0.0;
-        };
-        Pair s0, s1;
-        int j = lo + lane;
-#pragma unroll 1
-        for (; j + 7 * 32 < hi; j += 8 * 32) {
+        // eight entries from `first` on, `step` apart, those before `end`; infinities carry nothing
+        auto eight = [&](int first, int step, int end, double (&v)[8]) {
             float p[8], q[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = law_at<LAW16>(a.p, prow + j + 32 * i);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = mode == 0 ? law_at<LAW16>(a.q, qrow + j + 32 * i) : 0.f;
-            if (mode == 1) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = j + 32 * i == drop ? 0.f : p[i];
+            for (int i = 0; i < 8; ++i) {
+                const int j = first + i * step;
+                p[i] = j < end ? law_at<LAW16>(a.p, prow + j) : 0.f;
+                q[i] = mode == 0 && j < end ? law_at<LAW16>(a.q, qrow + j) : 0.f;
             }
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                s0.add(mass_of(p[i]), mass_of(q[i]));
-                s1.add(mass_of(p[i + 1]), mass_of(q[i + 1]));
+            for (int i = 0; i < 8; ++i) {
+                const float x = p[i] < INFINITY && !(mode == 1 && first + i * step == drop) ? p[i] : 0.f;
+                const Left l = left_of(x, q[i]);
+                v[i] = (double)l.d + (double)l.e;
             }
+        };
+        // 16 bytes a lane and load where both laws lie on such boundaries, four loads of each in flight
+        constexpr int EACH = LAW16 ? 8 : 4, SIZE = LAW16 ? 2 : 4;
+        Sum part;
+        int from = lo;
+        const char* pw = (const char*)a.p + (prow + lo) * SIZE;
+        const char* qw = mode == 0 ? (const char*)a.q + (qrow + lo) * SIZE : pw;
+        if (((((uintptr_t)pw) | ((uintptr_t)qw)) & 15) == 0) {
+            const int loads = (hi - lo) / (128 * EACH) * 4;
+#pragma unroll 1
+            for (int b0 = 0; b0 < loads; b0 += 4) {
+                uint4 p[4], q[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = __ldg(reinterpret_cast<const uint4*>(pw) + (b0 + i) * 32 + lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[i] = mode == 0 ? __ldg(reinterpret_cast<const uint4*>(qw) + (b0 + i) * 32 + lane) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int first = lo + ((b0 + i) * 32 + lane) * EACH;
+                    const uint32_t x[4] = {p[i].x, p[i].y, p[i].z, p[i].w}, y[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+                    if (mode == 1 && (unsigned)(drop - first) < (unsigned)EACH) continue;        // (added below, without the draft)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (LAW16) {
+                            part.add(left_of(bf16lo(x[e]), bf16lo(y[e])));
+                            part.add(left_of(bf16hi(x[e]), bf16hi(y[e])));
+                        } else {
+                            part.add(left_of(__uint_as_float(x[e]), __uint_as_float(y[e])));
+                        }
+                    }
+                }
+            }
+            from += loads * 32 * EACH;
         }
-        double rest = 0.0;
-        for (; j < hi; j += 32) rest += entry(j);
-        const double sum = warp_sum(s0.value() + s1.value() + rest);
+        double mass = part.value();
+        auto add_up = [&](int first, int end) {
+            for (int j = first + lane; j < end; j += 256) {
+                double v[8];
+                eight(j, 32, end, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) mass += v[i];
+            }
+        };
+        if (mode == 1 && drop >= lo && drop < from) {                    // the load that was left out
+            const int first = lo + (drop - lo) / EACH * EACH;
+            add_up(first, first + EACH);
+        }
+        add_up(from, hi);
+        double sum = warp_sum(mass);
+        if (!(sum < INFINITY)) {                                         // an infinite entry
+            mass = 0.0;
+            add_up(lo, hi);
+            sum = warp_sum(mass);
+        }
         const int form = mode == 2 ? 1 : 0;
         if (lane < ctas) {
             const uint32_t there = map_to_cta(smem_u32(&sums[form][mine]), (uint32_t)lane);
@@ -183,16 +223,21 @@ verify_kernel(const VerifyArgs a) {
             const double e = __shfl_sync(0xffffffffu, edge[i], past > 0 ? (past - 1) / (VSUMS / 32) : 0);
             if (past > 0 && (past - 1) % (VSUMS / 32) == i) left = e;
         }
-        // The CTA's warps take a stretch of that piece each.  Where another order of the sums leaves the target behind the last
-        // entry, it is the last entry that carries anything.
-        const int f0 = (int)((long long)past * V / all), len = (int)((long long)(past + 1) * V / all) - f0;
+        // The CTA's warps take a stretch of that piece each, in up to 32 blocks: a block's entries are summed side by side, lane b
+        // keeps the sum of block b.  Then the block that holds the target, a few neighbours a lane.  Where another order of the sums leaves
+        // the target behind the last entry, it is the last entry that carries anything.
+        const int f0 = piece(past), len = piece(past + 1) - f0;
         const int g0 = f0 + (int)((long long)warp * len / VW), g1 = f0 + (int)((long long)(warp + 1) * len / VW);
-        const int per = (g1 - g0 + 31) / 32, b0 = min(g0 + lane * per, g1), b1 = min(b0 + per, g1);
+        const int block = ((g1 - g0 + 8191) / 8192) * 256;
         double s = 0.0;
-#pragma unroll 8
-        for (int i = b0; i < b1; ++i) s += entry(i);
-        const double upto_lane = warp_scan(s, lane);
-        if (lane == 31) stretch[warp] = upto_lane;
+        for (int b = 0; g0 + b * block < g1; ++b) {
+            mass = 0.0;
+            add_up(g0 + b * block, min(g0 + (b + 1) * block, g1));
+            const double x = warp_sum(mass);
+            if (lane == b) s = x;
+        }
+        double upto_block = warp_scan(s, lane);
+        if (lane == 31) stretch[warp] = upto_block;
         __syncthreads();
         double want = target - left;
         int pick = -1, some = 0;
@@ -205,17 +250,36 @@ verify_kernel(const VerifyArgs a) {
         }
         if (pick < 0) { pick = some; want = INFINITY; }
         if (pick != warp) break;
-        const unsigned here = __ballot_sync(0xffffffffu, upto_lane > want && s > 0.0), any = __ballot_sync(0xffffffffu, s > 0.0);
-        const int winner = here ? __ffs(here) - 1 : 31 - __clz(any);
+        auto choose = [&](double upto_lane, double mine_sum) {           // the lane whose share holds the target, and what lies in front of it
+            const unsigned here = __ballot_sync(0xffffffffu, upto_lane > want && mine_sum > 0.0), any = __ballot_sync(0xffffffffu, mine_sum > 0.0);
+            const int winner = here ? __ffs(here) - 1 : 31 - __clz(any);
+            if (!here) want = INFINITY;
+            want -= __shfl_sync(0xffffffffu, upto_lane - mine_sum, winner);
+            return winner;
+        };
+        const int b = choose(upto_block, s), h0 = g0 + b * block, h1 = min(h0 + block, g1);
+        const int b0 = min(h0 + lane * (block / 32), h1), b1 = min(b0 + block / 32, h1);
+        s = 0.0;
+        double v[8];
+        for (int i = b0; i < b1; i += 8) {
+            eight(i, 1, b1, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += v[e];
+        }
+        const int winner = choose(warp_scan(s, lane), s);
         if (lane == winner) {
-            double run_x = upto_lane - s;
+            double reached = 0.0;
             int token = b0;
-            for (int i = b0; i < b1; ++i) {
-                const double x = entry(i);
-                if (!(x > 0.0)) continue;
-                token = i;
-                run_x += x;
-                if (run_x > want) break;
+            bool found = false;
+            for (int i = b0; i < b1 && !found; i += 8) {
+                eight(i, 1, b1, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (found || !(v[e] > 0.0)) continue;
+                    token = i + e;
+                    reached += v[e];
+                    found = reached > want;
+                }
             }
             out[at] = token;
         }

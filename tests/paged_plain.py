@@ -144,7 +144,7 @@ def verify(p, q, tokens, u, n):
             ok = u[i] * qx < p[i, x]
         if not ok:
             if q is not None:
-                left = np.maximum(mass(p[i]) - mass(q[i]), 0.0)
+                left = np.maximum(mass(p[i]) - np.where(q[i] > 0, q[i], 0.0), 0.0)        # (an infinite entry of q leaves nothing)
             else:
                 left = mass(p[i]).copy()
                 if 0 <= x < p.shape[1]:

@@ -95,6 +95,7 @@ def test_laws_without_mass(b):
     p4[:, :, 51] = float("inf")
     q4 = q.clone()
     q4[:, :, 300:] = float("nan")
+    q4[:, :, 7], q4[:, :, 9] = float("inf"), -0.25
     tok4 = torch.randint(0, 50, (8, 2), device="cuda").int()
     compare(b, p4, q4, tok4, u)
     p5 = torch.zeros_like(p)                         # one entry
