@@ -86,7 +86,7 @@ __device__ __forceinline__ u64 add2(u64 a, u64 b) { u64 r; asm("add.rn.f32x2 %0,
 __device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 // four e4m3 numbers times a power of two, `up` times `rest` less the 2^120 that the exponent fields lie apart, as two words of two bf16
 __device__ __forceinline__ uint2 widen4(uint32_t w, uint32_t up, uint32_t rest, bool twice) {
-    w = __byte_perm(w, 0, 0x3120);                               // numbers 0, 2, 1, 3
+    w = __byte_perm(w, 0, 0x3120);                               // numbers 0, 2, 1, 3 (never an infinity or NaN as they are put together here)
     uint32_t a = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u), b = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
     asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(up));
     asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(b) : "r"(up));
@@ -302,7 +302,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         unsigned n = 0;
         uint32_t landings = 0;                                   // parities of landed[]
         bool ok = true;
-        const int f = warp - 4, t128 = tid - 128;
+        const int f = warp - 4;
         while (unit < end && ok) {
             const ChunkPiece p(w, at, end, group);
             for (int t = p.first; t < p.stop && ok; ++t) {
@@ -353,32 +353,36 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                         const unsigned lost = bars.lost[n >> 1 & 7];
                         const unsigned char* raw = raws + stage * C::RAW;
                         const uint32_t dst = smem_u32(slots) + slot * C::TILE_BYTES;
-                        constexpr int PER = DH / 16, STEP = 128 / PER;   // 16-byte pieces of a row, rows a turn
-                        unsigned odd = 0;
+                        // 16-byte pieces of a row, rows a turn, of them a warp's; a lane works the scale of one of the warp's 32 rows out
+                        constexpr int PER = DH / 16, STEP = 128 / PER, MINE = 32 / PER;
+                        const int row = STEP * (lane / MINE) + MINE * f + lane % MINE;
+                        const unsigned e = raw[CH_KEYS * DH + row];
+                        // 2^(e - 127) times 2^120, as one power where that is one; 0 for what is not there; NaN for 255, but values that not
+                        // every row sees are taken out and put in at the end
+                        unsigned field = min(e + 120u, 254u), more = e + 120u > 254u ? e + 120u - 254u + 127u : 127u;
+                        uint32_t up = two_powers(field);
+                        bool odd = false;
+                        if (row >= left || (lost >> (row >> 4) & 1)) { up = 0u; more = 127u; }
+                        else if (e == 255u) {
+                            odd = kv && row >= see;
+                            up = odd ? 0u : 0x7fc07fc0u;
+                            more = 127u;
+                        }
+                        const bool twice = __any_sync(0xffffffffu, more != 127u);
+                        const uint32_t rest = two_powers(more);
+                        const int key0 = MINE * f + lane / PER, c = lane % PER;
+                        const unsigned char* src = raw + key0 * DH + 16 * c;
+                        const uint32_t d0 = dst + tile_off(key0, 2 * c, CH_KEYS), d1 = dst + tile_off(key0, 2 * c + 1, CH_KEYS);
 #pragma unroll 4
                         for (int i = 0; i < CH_KEYS / STEP; ++i) {
-                            const int key = i * STEP + t128 / PER, c = t128 % PER;
-                            const bool there = key < left && !(lost >> (key >> 4) & 1);
-                            uint4 u = *reinterpret_cast<const uint4*>(raw + key * DH + 16 * c);
-                            const unsigned e = raw[CH_KEYS * DH + key];
-                            // the scale 2^(e - 127) times 2^120, as one power where that is one
-                            unsigned field = min(e + 120u, 254u), more = e + 120u > 254u ? e + 120u - 254u + 127u : 127u;
-                            if (!there) u = make_uint4(0u, 0u, 0u, 0u), field = more = 127u;
-                            else if (e == 255u) {                // NaN; values that not every row sees are put in at the end
-                                field = 255u; more = 127u;
-                                if (kv && key >= see) { field = 0u; odd |= 1u << (key & 31); }
-                                u = field ? make_uint4(0u, 0u, 0u, 0u) : u;          // (0 x infinity)
-                            }
-                            const bool twice = __any_sync(0xffffffffu, more != 127u);
-                            const uint32_t up = two_powers(field), rest = two_powers(more);
-                            const uint2 x = widen4(u.x, up, rest, twice), y = widen4(u.y, up, rest, twice), z = widen4(u.z, up, rest, twice), v = widen4(u.w, up, rest, twice);
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + tile_off(key, 2 * c, CH_KEYS)), "r"(x.x), "r"(x.y), "r"(y.x), "r"(y.y) : "memory");
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(dst + tile_off(key, 2 * c + 1, CH_KEYS)), "r"(z.x), "r"(z.y), "r"(v.x), "r"(v.y) : "memory");
+                            const uint4 u = *reinterpret_cast<const uint4*>(src + i * STEP * DH);
+                            const uint32_t by1 = __shfl_sync(0xffffffffu, up, MINE * i + lane / PER), by2 = __shfl_sync(0xffffffffu, rest, MINE * i + lane / PER);
+                            const uint2 x = widen4(u.x, by1, by2, twice), y = widen4(u.y, by1, by2, twice), z = widen4(u.z, by1, by2, twice), v = widen4(u.w, by1, by2, twice);
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d0 + i * STEP * 128), "r"(x.x), "r"(x.y), "r"(y.x), "r"(y.y) : "memory");
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(d1 + i * STEP * 128), "r"(z.x), "r"(z.y), "r"(v.x), "r"(v.y) : "memory");
                         }
-                        if (kv) {
-                            odd = __reduce_or_sync(0xffffffffu, odd);    // (of positions anywhere in the tile: that some are is all that is asked)
-                            if (lane == 0) bars.odd[n >> 1 & 7][f] = odd;
-                        }
+                        const unsigned word = __ballot_sync(0xffffffffu, odd);       // (of positions anywhere in the tile: that some are is all that is asked)
+                        if (kv && lane == 0) bars.odd[n >> 1 & 7][f] = word;
                         fence_async_smem();
                         __syncwarp();
                         if (lane == 0) { mbar_arrive(&bars.rawfree[stage]); mbar_arrive(&bars.full[slot]); }
