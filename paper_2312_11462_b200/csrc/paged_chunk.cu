@@ -21,6 +21,7 @@
 namespace csd {
 
 constexpr int CH_KEYS = 128, CH_ROWS = 256, CH_THREADS = 512;
+constexpr int JOIN_MOST = 1024;                // CTAs at most
 constexpr int CH_MORE = 136, CH_FEWER = 120;     // registers of a softmax thread and of the others: 512 threads are launched with 128 each
 static_assert(256 * CH_MORE + 256 * CH_FEWER <= 512 * 128, "a setmaxnreg.inc beyond the launch's registers would wait for good");
 constexpr float CH_LATE = 16.f;                 // a running maximum may lag by this power of two (bf16 and fp32 have room for it)
@@ -37,10 +38,15 @@ template <int DH, bool E4M3> struct ChunkCfg {
     static constexpr int O_COL = 256;                            // tensor memory: S0, S1 (128 columns each), O0, O1
 };
 
+// An item whose parts lie in the workspace, by the CTA that has its first one; no part is looked at where `last` is below 0.
+struct alignas(32) ChunkJoin { int last, start, head, p0, rows, _[3]; };
+// (the workspace: the tickets of the other kernel, joins, parts)
+__host__ __device__ __forceinline__ ChunkJoin* joins_of(const AttendArgs& a) { return (ChunkJoin*)((char*)a.tickets + PAGED_TICKET_BYTES); }
+
 struct ChunkBars {
-    uint64_t full[8], free_[8], landed[8], rawfull[2], rawfree[2], qfull, qfree, sfull[2], pready[2][2], firsthalf[2], ofull[2], ofree[2], joined[2], told[2];
+    uint64_t full[8], free_[8], landed[8], rawfull[2], rawfree[2], qfull, qfree, sfull[2], pready[2][2], firsthalf[2], ofull[2], ofree[2];
     uint32_t tmem;
-    int abort_flag, last[2];
+    int abort_flag;
     // of the run's last eight position tiles: groups of 16 without a page; positions with values that were taken out
     unsigned lost[8], odd[8][4];
 };
@@ -160,6 +166,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, group = a.group;
 
     pdl_wait();
+    if (tid == 0) joins_of(a)[blockIdx.x].last = -1;             // (the barriers of the count lie before what the softmax warps write there)
     ChunkSchedule::count<CH_THREADS>(w, group, false, prefix);
     const u64 units = prefix[w.n_seqs];
     const unsigned n_runs = units < gridDim.x ? (unsigned)units : gridDim.x;
@@ -176,7 +183,6 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars.sfull[i], 1); mbar_init(&bars.pready[i][0], 4); mbar_init(&bars.pready[i][1], 4);
             mbar_init(&bars.firsthalf[i], 1); mbar_init(&bars.ofull[i], 1); mbar_init(&bars.ofree[i], 4);
-            mbar_init(&bars.joined[i], 4); mbar_init(&bars.told[i], 1);
         }
         bars.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -469,7 +475,7 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const uint32_t lanes = (uint32_t)(32 * quad) << 16, S = tmem + lanes + 128 * half, O = tmem + lanes + C::O_COL + 128 * half;
         const float to_log2 = a.scale * 1.4426950408889634f;
         const u64 by = two(to_log2, to_log2);
-        uint32_t done = 0, run_tiles = 0, joins = 0;             // position tiles of the half, of the run, items joined so far
+        uint32_t done = 0, run_tiles = 0;                        // position tiles of the half, of the run
         int rounds = 0;
         bool ok = true;
         while (unit < end && ok) {
@@ -634,54 +640,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             }
             if (!p.whole && p.nrows > 128 * half) {
                 if (mine) { __stcg(part + CH_ROWS * DH + r, m); __stcg(part + CH_ROWS * DH + CH_ROWS + r, l); }
-                // the half's last part to arrive adds them up, in the order of their runs
-                int c0, c1;
-                ChunkSchedule::parts_of(at, units, n_runs, snap, &c0, &c1);
-                __threadfence();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.joined[half]);
-                if (quad == 0) {
-                    ok = warp_waits(&bars.joined[half], joins & 1u);
-                    if (!ok) break;
-                    if (lane == 0) {
-                        bars.last[half] = atomicInc(a.tickets + 2 * c0 + half, (unsigned)(c1 - c0)) == (unsigned)(c1 - c0);
-                        mbar_arrive(&bars.told[half]);
-                    }
-                }
-                ok = warp_waits(&bars.told[half], joins++ & 1u);
-                if (!ok) break;
-                if (bars.last[half]) {
-                    __threadfence();
-                    auto of = [&](int c) { return a.parts + ((size_t)c * 2 + (c == c0 ? 1 : 0)) * C::PART; };
-                    float top = -INFINITY, total = 0.f;
-                    if (mine) {
-                        for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(of(c) + CH_ROWS * DH + r));
-                        const float base = top == -INFINITY ? 0.f : top;
-                        for (int c = c0; c <= c1; ++c) total += ex2(__ldcg(of(c) + CH_ROWS * DH + r) - base) * __ldcg(of(c) + CH_ROWS * DH + CH_ROWS + r);
-                        top = base;
-                    }
-                    const float scale = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll 1
-                    for (int c = 0; c < DH; c += 32) {
-                        float o[32];
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) o[j] = 0.f;
-                        float next_m = mine ? __ldcg(of(c0) + CH_ROWS * DH + r) : -INFINITY;
-#pragma unroll 1
-                        for (int k = c0; k <= c1; ++k) {
-                            const float pm = next_m;
-                            if (k < c1 && mine) next_m = __ldcg(of(k + 1) + CH_ROWS * DH + r);
-                            if (pm == -INFINITY) continue;       // (nothing was written of the row)
-                            const float* src = of(k) + (half * DH + c) * 128 + 32 * quad + lane;
-                            float x[32];
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) x[j] = __ldcg(src + j * 128);
-                            const float f = ex2(pm - top);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] = fmaf(f, x[j], o[j]);
-                        }
-                        store_rows(c, o, scale);
-                    }
+                if (r == 0 && p.first == 0) {                    // the item's first part tells of it
+                    int c0, c1;
+                    ChunkSchedule::parts_of(at, units, n_runs, snap, &c0, &c1);
+                    joins_of(a)[blockIdx.x] = ChunkJoin{c1, at.q.start, at.h, p.p0, p.nrows, {}};
                 }
             }
             run_tiles += (uint32_t)(p.stop - p.first);
@@ -700,6 +662,98 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     }
 }
 
+// Adds up the parts of the items that lie in several CTAs' runs, in the order of the runs.  The grid takes the items' jobs, 16 dimensions of a half's
+// 128 rows each, in turn: a warp two dimensions, a lane four rows, JOIN_PARTS parts under way at a time.  (Bounded by the parts' way through the
+// L2 cache. While the last CTA to arrive at an item added it up alone, 16 rows of 32 heads on 8 behind 16000 positions, 18 parts an item, took 74 us, 48 of
+// them for this; XX.)
+constexpr int JOIN_PARTS = 4, JOIN_DIMS = 16, JOIN_THREADS = 256;
+template <int DH> __global__ void __launch_bounds__(JOIN_THREADS, 2) paged_join_kernel(const AttendArgs a, int n) {
+    constexpr int PART = ChunkCfg<DH, false>::PART, GROUPS = DH / JOIN_DIMS, WARPS = JOIN_THREADS / 32;
+    static_assert(JOIN_DIMS == 2 * WARPS, "two dimensions a warp");
+    __shared__ int counts[WARPS];
+    __shared__ short items[JOIN_MOST];
+    __shared__ float outs[JOIN_DIMS][128 + 4];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const ChunkJoin* joins = joins_of(a);
+    pdl_wait();
+    pdl_trigger();
+    int n_items = 0;
+    for (int c0 = 0; c0 < n; c0 += JOIN_THREADS) {
+        const bool has = c0 + tid < n && __ldcg(&joins[c0 + tid].last) >= 0;
+        const unsigned in = __ballot_sync(0xffffffffu, has);
+        if (lane == 0) counts[warp] = __popc(in);
+        __syncthreads();
+        int at = n_items;
+        for (int i = 0; i < WARPS; ++i) {
+            if (i < warp) at += counts[i];
+            n_items += counts[i];
+        }
+        if (has) items[at + __popc(in & ((1u << lane) - 1u))] = (short)(c0 + tid);
+        __syncthreads();
+    }
+    for (int job = blockIdx.x; job < n_items * 2 * GROUPS; job += gridDim.x) {
+        const int c0 = items[job / (2 * GROUPS)], half = job / GROUPS & 1, d0 = job % GROUPS * JOIN_DIMS;
+        const int4 told = __ldcg(reinterpret_cast<const int4*>(joins + c0));
+        const ChunkJoin item = {told.x, told.y, told.z, told.w, __ldcg(&joins[c0].rows), {}};
+        const int rows = min(item.rows - 128 * half, 128);
+        if (rows <= 0) continue;
+        const int r = 4 * lane;                                  // (rows behind the item's are never written out)
+        float top[4], total[4], o[2][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { top[i] = -INFINITY; total[i] = o[0][i] = o[1][i] = 0.f; }
+        for (int k0 = c0; k0 <= item.last; k0 += JOIN_PARTS) {
+            float m[JOIN_PARTS][4], l[JOIN_PARTS][4], x[2][JOIN_PARTS][4];
+#pragma unroll
+            for (int k = 0; k < JOIN_PARTS; ++k) {
+                const bool there = k0 + k <= item.last && r < rows;
+                const float* part = a.parts + ((size_t)(k0 + k) * 2 + (k0 + k == c0 ? 1 : 0)) * PART;
+                auto get = [&](float (&to)[4], int at, float none) {
+                    const float4 v = there ? __ldcg(reinterpret_cast<const float4*>(part + at)) : make_float4(none, none, none, none);
+                    to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w;
+                };
+                get(m[k], CH_ROWS * DH + 128 * half + r, -INFINITY);
+                get(l[k], CH_ROWS * DH + CH_ROWS + 128 * half + r, 0.f);
+                get(x[0][k], (half * DH + d0 + 2 * warp) * 128 + r, 0.f);
+                get(x[1][k], (half * DH + d0 + 2 * warp + 1) * 128 + r, 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float now = top[i];
+#pragma unroll
+                for (int k = 0; k < JOIN_PARTS; ++k) now = fmaxf(now, m[k][i]);
+                const float keep = top[i] == -INFINITY ? 0.f : ex2(top[i] - now);
+                top[i] = now;
+                total[i] *= keep; o[0][i] *= keep; o[1][i] *= keep;
+#pragma unroll
+                for (int k = 0; k < JOIN_PARTS; ++k) {
+                    if (m[k][i] == -INFINITY) continue;          // (nothing was written of the row)
+                    const float f = ex2(m[k][i] - now);
+                    total[i] = fmaf(f, l[k][i], total[i]);
+                    o[0][i] = fmaf(f, x[0][k][i], o[0][i]);
+                    o[1][i] = fmaf(f, x[1][k][i], o[1][i]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float scale = total[i] == 0.f ? 0.f : 1.f / total[i];
+            outs[2 * warp][r + i] = o[0][i] * scale;
+            outs[2 * warp + 1][r + i] = o[1][i] * scale;
+        }
+        __syncthreads();
+        // two threads a row, eight dimensions each
+        const int row = tid >> 1, d = tid % 2 * 8;
+        if (row < rows) {
+            const int p = item.p0 + 128 * half + row;
+            uint32_t u[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = pack_bf16(outs[d + 2 * j][row], outs[d + 2 * j + 1][row]);
+            *reinterpret_cast<uint4*>((uint16_t*)a.out + (size_t)(item.start + p / a.group) * a.ldo + (size_t)(item.head * a.group + p % a.group) * DH + d0 + d) = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+        __syncthreads();
+    }
+}
+
 template <int DH, bool E4M3> static csd_status run_chunk(const PagedView& w, const AttendArgs& a, cudaStream_t st) {
     using C = ChunkCfg<DH, E4M3>;
     auto kern = paged_chunk_kernel<DH, E4M3>;
@@ -714,16 +768,20 @@ template <int DH, bool E4M3> static csd_status run_chunk(const PagedView& w, con
     PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(CH_THREADS), C::SMEM, st);
     CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, tk, tv, w, a));
     count_launch();
+    PdlLaunch J(dim3((unsigned)(2 * tc_sm_count())), dim3(JOIN_THREADS), 0, st);
+    CSD_CUDA(cudaLaunchKernelEx(&J.cfg, paged_join_kernel<DH>, a, tc_sm_count()));
+    count_launch();
     return CSD_OK;
 }
 
 size_t paged_chunk_workspace(int d_head) {
-    return PAGED_TICKET_BYTES + (size_t)tc_sm_count() * 2 * (d_head == 64 ? ChunkCfg<64, false>::PART : ChunkCfg<128, false>::PART) * 4;
+    return PAGED_TICKET_BYTES + JOIN_MOST * sizeof(ChunkJoin) + (size_t)tc_sm_count() * 2 * (d_head == 64 ? ChunkCfg<64, false>::PART : ChunkCfg<128, false>::PART) * 4;
 }
 
 csd_status launch_paged_chunk(const PagedView& w, AttendArgs a, int d_head, void* workspace, cudaStream_t st) {
+    if (tc_sm_count() > JOIN_MOST) return CSD_ERR_UNSUPPORTED;
     a.tickets = (unsigned*)workspace;
-    a.parts = (float*)((char*)workspace + PAGED_TICKET_BYTES);
+    a.parts = (float*)(joins_of(a) + JOIN_MOST);
     if (d_head == 64) return w.k_exp ? run_chunk<64, true>(w, a, st) : run_chunk<64, false>(w, a, st);
     return w.k_exp ? run_chunk<128, true>(w, a, st) : run_chunk<128, false>(w, a, st);
 }
