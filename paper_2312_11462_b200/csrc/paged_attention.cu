@@ -18,6 +18,13 @@ static int packed_rows(const csd_paged_batch* batch, const csd_kv_pool* pool, in
     return batch->max_rows * (n_heads / pool->n_kv_heads);
 }
 
+// Which kernel takes bf16 rows.  Up to 32 pairs are one or two blocks of 16 of the rows kernel, which then reads the cache once; from 33 on it
+// reads it several times, and the chunk kernel's block of 256 once.  32 heads on 8 of 128 dimensions, us in the rows and the chunk kernel:
+//   pairs   1 sequence x 16000   16 x 4000    64 x 2000
+//    16         28    34          57   85     104  144
+//    32         38    35          74   85     145  144
+//    48         52    33         135   87     268  146
+//   128         74    34         240   87     506  148
 static bool takes_chunks(int packed, int row_type) { return row_type == CSD_BF16 && packed > 32; }
 
 extern "C" size_t csd_paged_attention_workspace_bytes(const csd_kv_pool* pool, const csd_paged_batch* batch, int n_heads, int row_type) {

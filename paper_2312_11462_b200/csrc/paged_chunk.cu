@@ -13,6 +13,10 @@
 // positions; the first one's product runs under the other's exponentials.  A running maximum is only brought up when a score is above it by 2^16
 // (bf16 and fp32 have room for that), so that hardly a tile after an item's first waits for its maximum or rescales the output.
 //
+// An item's rows that lie in several CTAs' runs leave as parts, which paged_join_kernel adds up.  Measured: 890 TFLOP/s of bf16 pages, 755 of 8-bit ones
+// (592 heads of 64 rows behind 4288 positions, 128 dimensions), bounded by a half's chain of scores, exponentials and products: with a quarter of the
+// exponentials as polynomials on the multipliers it is 3 to 5 % slower, so the special-function unit is not what holds it up.
+//
 // What lies behind a sequence's positions may be anything, and 0 x NaN is NaN: values behind the last position are zeroed, and so
 // are infinities and NaN in positions that some of the block's rows do not see; rows that see them get them added at the end.
 #include "paged_attention.cuh"
@@ -663,11 +667,12 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 }
 
 // Adds up the parts of the items that lie in several CTAs' runs, in the order of the runs.  The grid takes the items' jobs, 16 dimensions of a half's
-// 128 rows each, in turn: a warp two dimensions, a lane four rows, JOIN_PARTS parts under way at a time.  (Bounded by the parts' way through the
-// L2 cache. While the last CTA to arrive at an item added it up alone, 16 rows of 32 heads on 8 behind 16000 positions, 18 parts an item, took 74 us, 48 of
-// them for this; XX.)
-constexpr int JOIN_PARTS = 4, JOIN_DIMS = 16, JOIN_THREADS = 256;
-template <int DH> __global__ void __launch_bounds__(JOIN_THREADS, 2) paged_join_kernel(const AttendArgs a, int n) {
+// 128 rows each, in turn: a warp two dimensions, a lane four rows, JOIN_PARTS parts under way at a time, three blocks an SM; it is bounded by the parts' way
+// through the L2 cache.  While the last CTA to arrive at an item added it up alone, 16 rows of 32 heads on 8 behind 16000 positions, 18 parts an item,
+// took 73 us, 48 of them for this, and behind 1000 32 us; now 35 and 17, and a prompt of 4096 rows, most items in two parts, 180 for 175.  (Four parts and two
+// blocks: 33, 17 and 186; two and four: 38, 18 and 184.)
+constexpr int JOIN_PARTS = 3, JOIN_DIMS = 16, JOIN_THREADS = 256;
+template <int DH> __global__ void __launch_bounds__(JOIN_THREADS, 3) paged_join_kernel(const AttendArgs a, int n) {
     constexpr int PART = ChunkCfg<DH, false>::PART, GROUPS = DH / JOIN_DIMS, WARPS = JOIN_THREADS / 32;
     static_assert(JOIN_DIMS == 2 * WARPS, "two dimensions a warp");
     __shared__ int counts[WARPS];
@@ -768,7 +773,7 @@ template <int DH, bool E4M3> static csd_status run_chunk(const PagedView& w, con
     PdlLaunch L(dim3((unsigned)tc_sm_count()), dim3(CH_THREADS), C::SMEM, st);
     CSD_CUDA(cudaLaunchKernelEx(&L.cfg, kern, tk, tv, w, a));
     count_launch();
-    PdlLaunch J(dim3((unsigned)(2 * tc_sm_count())), dim3(JOIN_THREADS), 0, st);
+    PdlLaunch J(dim3((unsigned)(3 * tc_sm_count())), dim3(JOIN_THREADS), 0, st);
     CSD_CUDA(cudaLaunchKernelEx(&J.cfg, paged_join_kernel<DH>, a, tc_sm_count()));
     count_launch();
     return CSD_OK;

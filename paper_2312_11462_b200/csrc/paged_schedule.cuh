@@ -2,7 +2,8 @@
 // for its queries and for its rows on their way out, and one for each of its key tiles.  The items' units lie one behind the other in the
 // order of the indices, and a CTA takes an equal run of them whatever the sequences' lengths are.  (Eight sequences of 77 to 2048
 // positions, trees of 12 rows, 32 heads, with tiles alone counted: 56 us, 37 where the lengths are even.)  A run that begins or ends inside an item
-// leaves its part of the item in the workspace, and the CTA that arrives last adds the parts up, in their order.
+// leaves its part of the item in the workspace, and the parts are added up in the order of the runs: by the CTA that arrives last (few rows), or by a
+// kernel behind this one (chunks).
 // A row of a row block is a (new row, query head of the group) pair: row p of the sequence's rows * group.
 #pragma once
 #include "paged.cuh"
@@ -17,7 +18,7 @@ struct AttendArgs {
     int group;                   // query heads a kv head
     float scale;
     RopeView rope;               // (fp32 rows alone)
-    unsigned* tickets;           // [CTAs]
+    unsigned* tickets;           // [CTAs]; behind them a chunk's joins
     float* parts;                // [CTAs][2] parts
 };
 
