@@ -28,6 +28,10 @@ constexpr int CH_KEYS = 128, CH_ROWS = 256, CH_THREADS = 512;
 constexpr int JOIN_MOST = 1024;                // CTAs at most
 constexpr int CH_MORE = 136, CH_FEWER = 120;     // registers of a softmax thread and of the others: 512 threads are launched with 128 each
 static_assert(256 * CH_MORE + 256 * CH_FEWER <= 512 * 128, "a setmaxnreg.inc beyond the launch's registers would wait for good");
+// Where every item can have a CTA of its own, it gets one, and no parts are added up, if the longest is not this many units above the even share.  (Prompt
+// of 1000 rows, 32 heads, 4 above: 32.7 us, 39.3 in even shares; 16 sequences of 16 rows behind 4000 positions, 5 above: 76 and 87; 8 behind 1000, 6: 27.5
+// and 29.9; 5 of 64 rows behind 1500 on 16 heads of 64, 7: 34.1 and 33.0; 256 rows behind 1000, 9: 36.3 and 29.5.)
+constexpr unsigned CH_ALONE = 6;
 constexpr float CH_LATE = 16.f;                 // a running maximum may lag by this power of two (bf16 and fp32 have room for it)
 
 template <int DH, bool E4M3> struct ChunkCfg {
@@ -50,7 +54,7 @@ __host__ __device__ __forceinline__ ChunkJoin* joins_of(const AttendArgs& a) { r
 struct ChunkBars {
     uint64_t full[8], free_[8], landed[8], rawfull[2], rawfree[2], qfull, qfree, sfull[2], pready[2][2], firsthalf[2], ofull[2], ofree[2];
     uint32_t tmem;
-    int abort_flag;
+    int abort_flag, longest;
     // of the run's last eight position tiles: groups of 16 without a page; positions with values that were taken out
     unsigned lost[8], odd[8][4];
 };
@@ -166,19 +170,26 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     unsigned char* slots = Qs + C::Q_BYTES;
     unsigned char* raws = slots + C::SLOTS * C::TILE_BYTES;
     u64* prefix = reinterpret_cast<u64*>(Qs);                    // (until the run's first unit is found)
-    static_assert((CSD_MAX_SEQS + 1) * 8 <= C::Q_BYTES, "the prefix fits");
+    static_assert(2 * (CSD_MAX_SEQS + 1) * 8 <= C::Q_BYTES, "the prefixes fit");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, group = a.group;
 
     pdl_wait();
     if (tid == 0) joins_of(a)[blockIdx.x].last = -1;             // (the barriers of the count lie before what the softmax warps write there)
-    ChunkSchedule::count<CH_THREADS>(w, group, false, prefix);
-    const u64 units = prefix[w.n_seqs];
-    const unsigned n_runs = units < gridDim.x ? (unsigned)units : gridDim.x;
-    if (blockIdx.x >= n_runs) return;
-    const int snap = ChunkSchedule::snap_of(units, n_runs, 3);
+    u64* items = prefix + CSD_MAX_SEQS + 1;
+    ChunkSchedule::count<CH_THREADS>(w, group, false, prefix, items, &bars.longest);
+    const u64 units = prefix[w.n_seqs], n_items = items[w.n_seqs];
     u64 begin, end;
     ChunkSchedule::Cursor at;
-    if (!ChunkSchedule::run(w, prefix, blockIdx.x, n_runs, snap, group, false, &begin, &end, &at)) return;
+    const unsigned n_runs = units < gridDim.x ? (unsigned)units : gridDim.x;
+    int snap = 0;
+    if (n_items <= gridDim.x && (u64)bars.longest <= units / gridDim.x + CH_ALONE) {
+        if (blockIdx.x >= n_items) return;
+        ChunkSchedule::item(w, items, blockIdx.x, group, false, &begin, &end, &at);
+    } else {
+        if (blockIdx.x >= n_runs) return;
+        snap = ChunkSchedule::snap_of(units, n_runs, 3);
+        if (!ChunkSchedule::run(w, prefix, blockIdx.x, n_runs, snap, group, false, &begin, &end, &at)) return;
+    }
 
     if (tid == 0) {
         for (int i = 0; i < 8; ++i) { mbar_init(&bars.full[i], 4); mbar_init(&bars.free_[i], 1); mbar_init(&bars.landed[i], 1); }

@@ -33,11 +33,32 @@ template <int BR, int KEYS, int OVER> struct Schedule {
         return (unsigned)(seen(w, q, rb, group, tree) + KEYS - 1) / KEYS;
     }
 
-    // prefix[s]: units before sequence s, prefix[n_seqs]: all of them.  THREADS threads; ends with a barrier.
+    // prefix[s]: units before sequence s, prefix[n_seqs]: all of them; with `items` the same of items, and in *longest the longest item's units.
+    // THREADS threads; ends with a barrier.
     template <int THREADS>
-    static __device__ void count(const PagedView& w, int group, bool tree, u64* prefix) {
+    static __device__ void count(const PagedView& w, int group, bool tree, u64* prefix, u64* items = nullptr, int* longest = nullptr) {
         __shared__ u64 warp_sums[THREADS / 32];
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+        if (items) {
+            u64 n = 0;
+            int most = 0;
+            for (int s = lane; warp == 0 && s < ((w.n_seqs + 31) & ~31); s += 32) {
+                PagedSeq q = {0, 0, 0};
+                if (s < w.n_seqs) q = paged_seq(w, s);
+                const int nb = blocks(q, group);
+                if (nb > 0) most = max(most, (int)tiles_of(w, q, nb - 1, group, tree) + OVER);
+                u64 x = (u64)nb * w.heads;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const u64 y = __shfl_up_sync(0xffffffffu, x, o);
+                    if (lane >= o) x += y;
+                }
+                if (s < w.n_seqs) items[s + 1] = n + x;
+                n += __shfl_sync(0xffffffffu, x, 31);
+            }
+            most = __reduce_max_sync(0xffffffffu, most);
+            if (tid == 0) { items[0] = 0; *longest = most; }
+        }
         u64 before = 0;
         for (int s0 = 0; s0 < w.n_seqs; s0 += THREADS) {
             const int s = s0 + tid;
@@ -174,6 +195,23 @@ template <int BR, int KEYS, int OVER> struct Schedule {
         if (*begin >= *end) return false;
         at->seek(w, prefix, *begin, group, tree);
         return true;
+    }
+    // Item i alone, as a run of its own.
+    static __device__ void item(const PagedView& w, const u64* items, unsigned i, int group, bool tree, u64* begin, u64* end, Cursor* at) {
+        int lo = 0, hi = w.n_seqs - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (items[mid] <= i) lo = mid; else hi = mid - 1;
+        }
+        const unsigned in = i - (unsigned)items[lo];
+        at->s = lo;
+        at->q = paged_seq(w, lo);
+        at->rb = (int)(in / (unsigned)w.heads);
+        at->h = (int)(in % (unsigned)w.heads);
+        at->block(w, group, tree);
+        at->item_first = *begin = 0;
+        at->tile = 0;
+        *end = at->item_end();
     }
     // The first and the last CTA that have a part of an item.
     static __device__ __forceinline__ void parts_of(const Cursor& at, u64 units, unsigned n, int snap, int* c0, int* c1) {

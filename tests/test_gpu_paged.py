@@ -127,6 +127,22 @@ def test_attention(b, kind, dtype, dim, page, rows, kv, heads, kv_heads):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("rows,kv,heads,kv_heads", [((20,), (6000,), 8, 2), ((300,), (2000,), 4, 2), ((40, 0, 1, 70), (900, 5, 0, 3000), 4, 2), ((129,), (4000,), 2, 1),
+                                                    ((33,) * 37, (70,) * 36 + (150,), 4, 4), ((33,) * 38, (70,) * 38, 4, 4), ((34, 0, 3) * 12, (5, 9, 300) * 12, 6, 6),
+                                                    ((50, 36), (0, 1200), 1, 1), ((1, 400), (2500, 2500), 2, 2)])
+def test_chunks_whole_and_in_parts(b, kind, dim, rows, kv, heads, kv_heads):
+    """Blocks of many rows whose items have CTAs of their own, and those that lie in up to dozens of parts; twice on one workspace."""
+    c = pp.Case(b, rows, kv, kv_heads, dim, 32, kind, BF16, seed=sum(rows) + dim, lead_rows=2)
+    c.fill()
+    ws = b.csd_paged_attention_workspace(c.pool, c.batch(), heads, BF16)
+    ws[4096:] = 0xff                                   # (what is behind the tickets may be anything)
+    one = attend(b, c, heads, ws=ws)
+    assert torch.equal(one.nan_to_num(), attend(b, c, heads, ws=ws).nan_to_num())
+    assert b.csd_device_status() == 0
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("rows,kv,heads,kv_heads", [((12, 5, 1), (77, 0, 300), 4, 4), ((64, 33), (0, 40), 4, 2), ((17,), (16,), 8, 1)])
 def test_trees(b, kind, dtype, rows, kv, heads, kv_heads):
