@@ -338,7 +338,8 @@ csd_status csd_paged_read(const csd_kv_pool* pool, const csd_paged_batch* batch,
  * of the same sequence's chunk; max_rows <= 64).  A row that sees nothing is 0.  q_dev [total_rows, n_heads * d_head], rows ldq
  * elements apart, out_dev likewise with ldo (multiples of 8; 16-byte aligned; out may not overlap q).  n_heads is a multiple of
  * the pool's kv heads, at most 64 times as many; query head h reads kv head h / (n_heads / n_kv_heads).  Scores, softmax and sums are fp32; bf16 rows enter the products as they are
- * and their weights as bf16, fp32 rows and weights as three bf16 terms each.
+ * and their weights as bf16; fp32 rows and weights as three bf16 terms each (rows over 8-bit keys as two fp16 terms, 22 bits).
+ * Infinities and NaN in the cache reach the rows that see them and no others.
  * The workspace has to be zero before its first call; every call leaves it ready for the next, of any shape.  Calls that may overlap
  * on the GPU need workspaces of their own. */
 size_t csd_paged_attention_workspace_bytes(const csd_kv_pool* pool, const csd_paged_batch* batch, int n_heads, int row_type);
