@@ -268,7 +268,7 @@ csd_status csd_spec_accept_static(const float* target_logits_dev, const float* d
  * on the differences of the given numbers; laws need not sum to 1.  Negative entries and NaN count as 0, an infinite
  * entry of p carries no mass, one of q leaves none.  A law without any mass gives token 0.
  *   target_probs_dev [rows, k+1, V], draft_probs_dev [rows, k, V] of prob_type (csd_row_type), consecutive laws ld_p and ld_q
- *   entries apart (>= V); draft_tokens_dev [rows, k] int32 (0 <= k <= 64); uniforms_dev [rows, k+1] fp32 in [0, 1): one a draft,
+ *   entries apart (>= V; V <= 2^30); draft_tokens_dev [rows, k] int32 (0 <= k <= 64); uniforms_dev [rows, k+1] fp32 in [0, 1): one a draft,
  *   the last for the output token.  Outputs: n_accepted_dev [rows]; tokens_dev [rows, k+1]: the accepted drafts, the output
  *   token, and -1 behind it.
  * A token id outside [0, V) is rejected and sets the device status to CSD_ERR_BAD_TOKEN, a count outside [0, k] is taken as

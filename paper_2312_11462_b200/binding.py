@@ -213,14 +213,20 @@ class Model:
         assert len(pools) == self.shape.n_layers
         if workspace is None:
             workspace = csd_paged_attention_workspace(pools[0], batch, self.shape.n_heads, torch.float32)
+        index = block_tokens.get_device()
+        assert batch.index == index and all(p.index == index for p in pools)
+        assert workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.get_device() == index
         if append_only:
             logits_out = None
         elif logits_out is None:
             logits_out = torch.empty(batch.total_rows, self.shape.vocab, dtype=torch.float32, device=block_tokens.device)
+        if logits_out is not None:
+            assert logits_out.dtype == torch.float32 and logits_out.is_contiguous() and logits_out.get_device() == index
+            assert logits_out.numel() == batch.total_rows * self.shape.vocab
         if tree_mask is not None:
-            assert tree_mask.dtype == torch.int64 and tree_mask.is_contiguous() and tree_mask.numel() == batch.total_rows
+            assert tree_mask.dtype == torch.int64 and tree_mask.is_contiguous() and tree_mask.numel() == batch.total_rows and tree_mask.get_device() == index
         structs = (KvPoolStruct * len(pools))(*[p.c for p in pools])
-        _call("csd_review_forward_paged", lib.csd_review_forward_paged, block_tokens.get_device(), self.h, C.addressof(structs), batch.ref,
+        _call("csd_review_forward_paged", lib.csd_review_forward_paged, index, self.h, C.addressof(structs), batch.ref,
               block_tokens.data_ptr(), _ptr(tree_mask), _ptr(logits_out), workspace.data_ptr(), workspace.numel())
         return logits_out
 

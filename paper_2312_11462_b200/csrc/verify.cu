@@ -316,10 +316,11 @@ using namespace csd;
 extern "C" csd_status csd_spec_verify(const void* target_probs_dev, int64_t ld_p, const void* draft_probs_dev, int64_t ld_q, int prob_type,
                                       const int32_t* draft_tokens_dev, const int32_t* n_drafts_dev, const float* uniforms_dev, int rows,
                                       int k, int V, int32_t* n_accepted_dev, int32_t* tokens_dev, void* stream) {
-    if (rows < 0 || rows > 1 << 24 || k < 0 || k > 64 || V < 1 || (prob_type != CSD_F32 && prob_type != CSD_BF16)) return CSD_ERR_INVALID_ARG;
+    if (rows < 0 || rows > 1 << 24 || k < 0 || k > 64 || V < 1 || V > 1 << 30 || (prob_type != CSD_F32 && prob_type != CSD_BF16)) return CSD_ERR_INVALID_ARG;
     if (rows == 0) return CSD_OK;
     if (!target_probs_dev || (k > 0 && !draft_tokens_dev) || !uniforms_dev || !n_accepted_dev || !tokens_dev) return CSD_ERR_INVALID_ARG;
     if (ld_p < V || (draft_probs_dev && ld_q < V)) return CSD_ERR_INVALID_ARG;
+    if (((uintptr_t)target_probs_dev | (uintptr_t)draft_probs_dev) & (prob_type == CSD_BF16 ? 1 : 3)) return CSD_ERR_INVALID_ARG;
     VerifyArgs a{target_probs_dev, draft_probs_dev, draft_tokens_dev, n_drafts_dev, uniforms_dev, n_accepted_dev, tokens_dev,
                  status_word_device(), ld_p, ld_q, k, V};
     if (!a.status) return CSD_ERR_CUDA;

@@ -115,6 +115,8 @@ def test_verify(b):
     for kw in (dict(rows=-1), dict(k=-1), dict(k=65), dict(V=0), dict(type=2), dict(type=-1), dict(p=None), dict(x=None), dict(u=None), dict(a=None), dict(out=None),
                dict(ldp=63), dict(ldq=63)):
         assert call(**kw) == INVALID, kw
+    for kw in (dict(V=(1 << 30) + 1, ldp=1 << 31, ldq=1 << 31), dict(p=4098), dict(q=4097, type=1)):      # too wide, laws between their entries' boundaries
+        assert call(**kw) == INVALID, kw
     assert b.lib.csd_status_string(9) == b"page id outside the pool"
 
 
