@@ -5,8 +5,8 @@
 // rn_e4m3(x * 2^-e).  The scale is a power of two, so x * 2^-e is exact and the result does not depend on how it is formed.
 //
 // A thread holds 8 neighbouring elements of one row, d_head / 8 threads a row, K and V of a head side by side; a warp belongs to
-// one position and looks it up once.  What bounds both directions is the row traffic: some 9000 positions of 32 heads x 128, bf16 to 8 bits and
-// back, 103 us, 77 % of the copy rate; reading 36000 positions of 8 heads alone 40 us, 88 %.
+// one position and looks it up once.  What bounds both directions is the row traffic: some 10500 positions of 32 heads x 128, bf16 to 8 bits and
+// back, 103 us, 77 % of the copy rate; reading 37500 positions of 8 heads alone 40 us, 88 %.
 #include "paged_attention.cuh"
 #include "tc_common.cuh"
 #include <cuda_fp8.h>
@@ -214,7 +214,7 @@ paged_read_kernel(const PagedView w, const RowsView dst, int split) {
 template <template <int, bool, bool> class Pick>
 static csd_status launch_cache(const PagedView& w, const RowsView& rows, int d_head, bool rows16, cudaStream_t st) {
     // warps a position: all its stretches at once while that leaves SMs idle, down to one, which looks up where the position lies
-    // once for all of them (9000 positions of 32 heads x 128, bf16 to 8 bits and back: 184 us with a warp a stretch, 149 so)
+    // once for all of them (10500 positions of 32 heads x 128, bf16 to 8 bits and back: 184 us with a warp a stretch, 149 so)
     const int stretches = (2 * w.heads * (d_head / 8) + 31) / 32;
     int split = stretches;
     while (split > 1 && (long long)w.total_rows * ((split + 1) / 2) >= 48ll * tc_sm_count()) split = (split + 1) / 2;
