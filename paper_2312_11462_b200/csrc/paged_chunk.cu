@@ -742,7 +742,9 @@ template <int DH> __global__ void __launch_bounds__(JOIN_THREADS, 3) paged_join_
                 total[i] *= keep; o[0][i] *= keep; o[1][i] *= keep;
 #pragma unroll
                 for (int k = 0; k < JOIN_PARTS; ++k) {
-                    if (m[k][i] == -INFINITY) continue;          // (nothing was written of the row)
+                    // nothing was written of the row, or it sees nothing in the part.  (Scores that are all NaN leave the maximum at -inf too, but
+                    // not the sum at 0: their NaN goes on.)
+                    if (m[k][i] == -INFINITY && l[k][i] == 0.f) continue;
                     const float f = ex2(m[k][i] - now);
                     total[i] = fmaf(f, l[k][i], total[i]);
                     o[0][i] = fmaf(f, x[0][k][i], o[0][i]);

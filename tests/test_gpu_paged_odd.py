@@ -1,0 +1,80 @@
+"""NaN and infinities in queries and in the paged cache: they reach the rows that see them, however the work is divided, and no others."""
+import numpy as np
+import pytest
+import torch
+
+import paged_plain as pp
+from gpu_util import require_gpu
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def b():
+    require_gpu()
+    from paper_2312_11462_b200 import binding
+    return binding
+
+
+def attend(b, c, q, masks=None):
+    """The operator on a filled case, beside the plain form: what is not finite lies in the same places and is the same, the rest is within the
+    bound of finite numbers (the scores' size is taken over the finite entries)."""
+    out = torch.full((c.total, q[0].shape[1], c.D), -7.0, dtype=c.dtype, device="cuda")
+    tm = None if masks is None else torch.tensor(masks + [0] * (c.total - len(masks)), dtype=torch.int64).cuda()
+    b.csd_paged_attention(c.packed(q), c.pool, c.batch(), tree_mask=tm, out=out)
+    got = out.double().cpu().numpy()
+    tame = lambda x: np.where(np.isfinite(x), x, 0.0)  # noqa: E731
+    for s, (r, n) in enumerate(zip(c.rows, c.kv)):
+        if not r:
+            continue
+        mine = None if masks is None else masks[c.start[s]:c.start[s + 1]]
+        qs, k, v = q[s].to(c.dtype).double().numpy(), c.held(c.keys[s]), c.held(c.vals[s])
+        with np.errstate(invalid="ignore"):
+            want, size, _ = pp.attention(qs, k, v, n, c.D ** -0.5, mine)
+        top = float(np.abs(tame(qs)).sum(-1).max() * np.abs(tame(k)).max() * c.D ** -0.5)
+        far, fine = got[c.start[s]:c.start[s + 1]], np.isfinite(want)
+        assert np.array_equal(np.isnan(want), np.isnan(far)), (s, int(np.isnan(want).sum()), int(np.isnan(far).sum()))
+        assert np.array_equal(np.where(np.isinf(want), want, 0), np.where(np.isinf(far), far, 0)), s
+        bound = pp.attention_bound(tame(want), tame(size), top, n + r, c.D, c.dtype)
+        assert (np.abs(np.where(fine, far, 0) - tame(want)) <= bound).all(), s
+    assert b.csd_device_status() == 0
+    return got
+
+
+# items with CTAs of their own, and items that lie in parts of a tile each and of several
+DIVISIONS = [((40, 40), (30, 100), 2, 1), ((300,), (20,), 4, 2), ((40,), (985,), 1, 1), ((300,), (2005,), 4, 2), ((70, 129), (6075, 4096), 2, 1)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("rows,kv,heads,kv_heads", DIVISIONS)
+def test_a_query_with_a_nan(b, kind, dim, rows, kv, heads, kv_heads):
+    """Its head's row is NaN, whole or in parts; all others are what they are without it."""
+    c = pp.Case(b, rows, kv, kv_heads, dim, 32, kind, BF16, seed=sum(rows))
+    c.fill()
+    g = torch.Generator().manual_seed(5)
+    q = [torch.randn(r, heads, dim, generator=g) for r in rows]
+    for x in q:
+        x[len(x) // 3, 0, 7] = float("nan")
+        x[-1, -1] = float("nan")
+    got = attend(b, c, q)
+    for s, x in enumerate(q):
+        assert np.isnan(got[c.start[s] + len(x) // 3, 0]).all() and np.isnan(got[c.start[s + 1] - 1, -1]).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,kv,heads,kv_heads", [((40,), (985,), 1, 1), ((40,), (89,), 1, 1), ((300,), (1877,), 2, 2), ((33, 65), (3040, 1600), 2, 2), ((1,), (2048,), 1, 1),
+                                                    ((7,), (1530,), 2, 1)])
+def test_a_nan_that_is_the_only_key_of_a_part(b, kind, dtype, rows, kv, heads, kv_heads):
+    """The newest position is the first of a tile of keys and a NaN: its own row, which sees nothing else in that tile, is NaN."""
+    c = pp.Case(b, rows, kv, kv_heads, 128, 64, kind, dtype, seed=sum(kv))
+    for k in c.keys:
+        k[-1, :, 3] = float("nan")
+    c.fill()
+    g = torch.Generator().manual_seed(6)
+    q = [torch.randn(r, heads, 128, generator=g) for r in rows]
+    got = attend(b, c, q)
+    for s in range(len(rows)):
+        assert np.isnan(got[c.start[s + 1] - 1]).all() and not np.isnan(got[c.start[s]:c.start[s + 1] - 1]).any()
