@@ -314,7 +314,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a) {
                 // ---- scale and mask; the warp's own running maxima
                 const bool edge = t0 + WK > all_see || gone;
                 float mx[MT][2];
-                bool grown = false;
+                bool grown = false, nan = false;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -332,7 +332,42 @@ paged_rows_kernel(const PagedView w, const AttendArgs a) {
                                     const bool sees = t < lim[mt][hr] || (back >= 0 && back < 64 && t < at.seen && (bits[mt][hr] >> back & 1));
                                     if (!sees || (gone >> (g >> 1) & 1)) x = -INFINITY;
                                 }
+                                nan |= x != x;
                             }
+                    }
+                // An infinite entry of a key times a query's smaller terms, 0 or of the other sign, is NaN or the other infinity: of fp32 rows
+                // the scores that are NaN are formed anew, each query entry as one number
+                if constexpr (!ROWS16 && !E4M3) {
+                    if (__any_sync(0xffffffffu, nan)) {
+                        const unsigned char* kt = stages + slot * C::STAGE;
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (int hr = 0; hr < 2; ++hr)
+#pragma unroll
+                                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        float& x = s[mt][g][2 * hr + e];
+                                        if (x == x) continue;
+                                        const int r = 16 * mt + (lane >> 2) + 8 * hr, k = 8 * g + 2 * (lane & 3) + e;
+                                        x = 0.f;
+#pragma unroll 1
+                                        for (int d = 0; d < DH; ++d) {
+                                            float y = 0.f;
+#pragma unroll
+                                            for (int t = 0; t < C::QT; ++t)
+                                                y += bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(Qs + (size_t)t * BR * DH * 2 + stage_off<2 * DH>(r, d >> 3) + 2 * (d & 7)));
+                                            x = fmaf(y, bf16_bits_to_float(*reinterpret_cast<const uint16_t*>(kt + stage_off<RB>(k, d >> 3) + 2 * (d & 7))), x);
+                                        }
+                                        x *= q_scale[mt][hr];
+                                    }
+                    }
+                }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int hr = 0; hr < 2; ++hr) {
                         float top = -INFINITY;
 #pragma unroll
                         for (int g = 0; g < NG; ++g) top = fmaxf(top, fmaxf(s[mt][g][2 * hr], s[mt][g][2 * hr + 1]));

@@ -78,3 +78,28 @@ def test_a_nan_that_is_the_only_key_of_a_part(b, kind, dtype, rows, kv, heads, k
     got = attend(b, c, q)
     for s in range(len(rows)):
         assert np.isnan(got[c.start[s + 1] - 1]).all() and not np.isnan(got[c.start[s]:c.start[s + 1] - 1]).any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("rows,kv,heads,kv_heads,tree", [((1, 1), (40, 500), 2, 1, False), ((5, 3), (300, 77), 4, 4, False), ((9, 12), (20, 0), 4, 2, True),
+                                                         ((60,), (700,), 2, 1, False), ((300,), (2005,), 2, 2, False),
+                                                         ((1, 2), (600, 20), 8, 4, False)])
+def test_infinite_keys(b, dtype, dim, rows, kv, heads, kv_heads, tree):
+    """A score of -inf is no weight, one of +inf makes its row NaN, whatever terms a query enters the products in."""
+    c = pp.Case(b, rows, kv, kv_heads, dim, 16, "bf16", dtype, seed=3)
+    for k, n in zip(c.keys, c.kv):
+        k[2 * len(k) // 3, 0, 1] = float("inf")
+        k[len(k) // 4, -1, 2] = -float("inf")
+        k[-1, 0, dim - 1] = float("inf")
+    c.fill()
+    masks = pp.trees(rows, 9) if tree else None
+    g = torch.Generator().manual_seed(7)
+    q = [torch.randn(r, heads, dim, generator=g) for r in rows]
+    for x in q:                                       # (most rows: scores of -inf alone)
+        x[..., [1, dim - 1]] = -x[..., [1, dim - 1]].abs()
+        x[..., 2].abs_()
+        x[len(x) // 2, 0, 1] = 1.7
+        x[-1, -1, 2] = -0.3
+    got = attend(b, c, q, masks)
+    assert np.isnan(got[:c.start[-1]]).any()
