@@ -407,8 +407,9 @@ paged_rows_kernel(const PagedView w, const AttendArgs a) {
                                 const float xr = bf16lo(u), yr = bf16hi(u);
                                 x -= xr; y -= yr;
                                 sum += xr + yr;
-                                // (a power of two: exact; a position that nobody sees may have any scale)
-                                if constexpr (E4M3) u = pack_bf16(x0 == 0.f ? 0.f : xr * vscale[g][0], y0 == 0.f ? 0.f : yr * vscale[g][1]);
+                                // (a power of two: exact; a position that nobody sees may have any scale, of one that all see a NaN counts even
+                                // where the weight is below fp32's range)
+                                if constexpr (E4M3) u = pack_bf16(edge && x0 == 0.f ? 0.f : xr * vscale[g][0], edge && y0 == 0.f ? 0.f : yr * vscale[g][1]);
                                 pa[mt][q][t][f] = u;
                             }
                             l[mt][hr] += sum;

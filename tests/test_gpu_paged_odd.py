@@ -103,3 +103,16 @@ def test_infinite_keys(b, dtype, dim, rows, kv, heads, kv_heads, tree):
         x[-1, -1, 2] = -0.3
     got = attend(b, c, q, masks)
     assert np.isnan(got[:c.start[-1]]).any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,heads", [(1, 1), (3, 2), (20, 1), (50, 2)])
+def test_a_nan_of_hardly_any_weight(b, kind, dtype, rows, heads):
+    """Values that are NaN reach every row that sees them, also where the weight is below fp32's range."""
+    c = pp.Case(b, (rows,), (700,), 1, 128, 32, kind, dtype, seed=rows)
+    c.keys[0][5] = -30.0
+    c.vals[0][5] = float("nan")
+    c.fill()
+    got = attend(b, c, [torch.ones(rows, heads, 128)])
+    assert np.isnan(got[:rows]).all()
