@@ -188,46 +188,47 @@ verify_kernel(const VerifyArgs a) {
             asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(there), "d"(sum) : "memory");
         }
         cluster_barrier();
-        // every warp: the pieces' edges, four a lane, the whole, and the piece that holds the target
-        double edge[VSUMS / 32], run = 0.0;
+        // every warp: where the pieces begin, two a lane, the whole, and the piece that holds the target: the last one with any mass that begins
+        // at or before it.  (Pieces that end before the target would do if sums were exact.  But a lane adds to the scan's
+        // sum, and the scan's next sum is added up in another order: the end of an empty piece can lie a rounding above the one before, and
+        // with the target between the two nothing would be chosen.)
+        double start[VSUMS / 32], run = 0.0;
+        bool some_of[VSUMS / 32];
 #pragma unroll
         for (int i = 0; i < VSUMS / 32; ++i) {
             const int w = lane * (VSUMS / 32) + i;
-            run += w < all ? sums[form][w] : 0.0;
-            edge[i] = run;
+            const double x = w < all ? sums[form][w] : 0.0;
+            some_of[i] = x > 0.0;
+            start[i] = run;
+            run += x;
         }
         const double upto = warp_scan(run, lane), before = __shfl_up_sync(0xffffffffu, upto, 1);
         const double base = lane ? before : 0.0;
-        double total = 0.0;
-#pragma unroll
-        for (int i = 0; i < VSUMS / 32; ++i) {
-            edge[i] += base;
-            total = edge[i];
-        }
-        total = __shfl_sync(0xffffffffu, total, 31);
+        const double total = __shfl_sync(0xffffffffu, base + run, 31);
         if (!(total > 0.0)) {
             if (mode != 2) continue;                 // nothing is left: the target's own law
             if (rank == 0 && tid == 0) out[at] = 0;
             break;
         }
         const double target = u * total;
-        // pieces that end at or before the target
-        int past = 0;
-#pragma unroll
-        for (int i = 0; i < VSUMS / 32; ++i) past += edge[i] <= target ? 1 : 0;
-        past = __reduce_add_sync(0xffffffffu, past);
-        if (past / VW != rank) break;                // (the same for all warps of a CTA)
-        // edge[] of the piece before that one
-        double left = 0.0;
+        int chosen = 0;                              // (the first piece with mass begins at 0)
 #pragma unroll
         for (int i = 0; i < VSUMS / 32; ++i) {
-            const double e = __shfl_sync(0xffffffffu, edge[i], past > 0 ? (past - 1) / (VSUMS / 32) : 0);
-            if (past > 0 && (past - 1) % (VSUMS / 32) == i) left = e;
+            start[i] += base;
+            if (some_of[i] && start[i] <= target) chosen = lane * (VSUMS / 32) + i;
+        }
+        chosen = __reduce_max_sync(0xffffffffu, chosen);
+        if (chosen / VW != rank) break;              // (the same for all warps of a CTA)
+        double left = 0.0;                           // in front of the piece
+#pragma unroll
+        for (int i = 0; i < VSUMS / 32; ++i) {
+            const double e = __shfl_sync(0xffffffffu, start[i], chosen / (VSUMS / 32));
+            if (chosen % (VSUMS / 32) == i) left = e;
         }
         // The CTA's warps take a stretch of that piece each, in up to 32 blocks: a block's entries are summed side by side, lane b
         // keeps the sum of block b.  Then the block that holds the target, a few neighbours a lane.  Where another order of the sums leaves
         // the target behind the last entry, it is the last entry that carries anything.
-        const int f0 = piece(past), len = piece(past + 1) - f0;
+        const int f0 = piece(chosen), len = piece(chosen + 1) - f0;
         const int g0 = f0 + (int)((long long)warp * len / VW), g1 = f0 + (int)((long long)(warp + 1) * len / VW);
         const int block = ((g1 - g0 + 8191) / 8192) * 256;
         double s = 0.0;
