@@ -265,8 +265,9 @@ csd_status csd_spec_accept_static(const float* target_logits_dev, const float* d
  * u_i * q_i(x_i) < p_i(x_i); at the first rejection i the output token is drawn from max(0, p_i - q_i) (from p_i
  * where that carries nothing), if all n are accepted from p_n.  draft_probs_dev NULL: point masses, q_i(x_i) = 1 and
  * 0 elsewhere.  The draw is the inverse CDF in vocabulary order, smallest j with cumulative mass > u_k * total, in fp64
- * on the differences of the given numbers; laws need not sum to 1.  Negative entries and NaN count as 0, an infinite
- * entry of p carries no mass, one of q leaves none.  A law without any mass gives token 0.
+ * on the differences of the given numbers; laws need not sum to 1.  Negative entries and NaN count as 0, in the tests of
+ * the drafts too (which compare infinities as they are); in a draw an infinite entry of p carries no mass, one of q leaves none.
+ * A law without any mass gives token 0.
  *   target_probs_dev [rows, k+1, V], draft_probs_dev [rows, k, V] of prob_type (csd_row_type), consecutive laws ld_p and ld_q
  *   entries apart (>= V; V <= 2^30); draft_tokens_dev [rows, k] int32 (0 <= k <= 64); uniforms_dev [rows, k+1] fp32 in [0, 1): one a draft,
  *   the last for the output token.  Outputs: n_accepted_dev [rows]; tokens_dev [rows, k+1]: the accepted drafts, the output

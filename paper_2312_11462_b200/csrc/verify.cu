@@ -84,8 +84,8 @@ verify_kernel(const VerifyArgs a) {
                 if (x < 0 || x >= V) {
                     stop = true;
                 } else {
-                    const float px = law_at<LAW16>(a.p, ((size_t)row * (k + 1) + i) * a.ldp + x);
-                    const float qx = a.q ? law_at<LAW16>(a.q, ((size_t)row * k + i) * a.ldq + x) : 1.f;
+                    const float px = fmaxf(law_at<LAW16>(a.p, ((size_t)row * (k + 1) + i) * a.ldp + x), 0.f);      // (negative numbers and NaN: 0)
+                    const float qx = a.q ? fmaxf(law_at<LAW16>(a.q, ((size_t)row * k + i) * a.ldq + x), 0.f) : 1.f;
                     stop = !((double)uniform(i, true) * (double)qx < (double)px);
                 }
             }

@@ -47,3 +47,25 @@ def test_a_target_beside_pieces_that_hold_nothing(b, first, others, into):
         b.csd_spec_verify(law.expand(1, 2, V).contiguous(), laws, draft, half, out=out)
         assert int(out[0]) == 0 and int(out[1][0, 0]) in fine and int(out[1][0, 1]) == -1
     assert b.csd_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_drafts_whose_entries_are_negative_or_not_numbers(b, dtype):
+    """They count as 0 in the tests of the drafts: accepted iff u * max(q, 0) < max(p, 0), a NaN as 0."""
+    nan, inf = float("nan"), float("inf")
+    #        p     q    u   accepted
+    cases = [(0.0, -0.5, 0.5, 0), (0.25, -0.5, 0.5, 1), (0.0, nan, 0.5, 0), (0.25, nan, 0.5, 1), (-0.25, -0.5, 0.5, 0), (-0.25, 0.5, 0.0, 0), (nan, 0.5, 0.5, 0),
+             (nan, nan, 0.5, 0), (nan, -0.5, 0.5, 0), (0.25, 0.5, 0.5, 0), (0.25, 0.375, 0.5, 1), (0.0, 0.0, 0.5, 0), (0.25, inf, 0.5, 0), (inf, 0.5, 0.5, 1), (inf, inf, 0.5, 0)]
+    n, x = len(cases), 5
+    p, q = torch.zeros(n, 2, 40), torch.zeros(n, 1, 40)
+    p[..., 9] = 0.5                                   # (the output token, after a rejection and behind the draft)
+    for i, (px, qx, _, _) in enumerate(cases):
+        p[i, 0, x], q[i, 0, x] = px, qx
+    u = torch.tensor([[c[2], 0.25] for c in cases], device="cuda")
+    tok = torch.full((n, 1), x, dtype=torch.int32, device="cuda")
+    a, out = b.csd_spec_verify(p.to(dtype).cuda(), q.to(dtype).cuda(), tok, u)
+    assert a.tolist() == [c[3] for c in cases] and b.csd_device_status() == 0
+    assert out.tolist() == [[x, 9] if c[3] else [9, -1] for c in cases]
+    a, out = b.csd_spec_verify(p.to(dtype).cuda(), None, tok, u)                # point masses: q = 1
+    want = [int(c[0] > c[2]) for c in cases]
+    assert a.tolist() == want and out.tolist() == [[x, 9] if w else [9, -1] for w in want] and b.csd_device_status() == 0
