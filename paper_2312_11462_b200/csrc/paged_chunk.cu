@@ -456,8 +456,10 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                     const uint64_t vt = vd + (uint64_t)(v * (C::TILE_BYTES >> 4));
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
+                        // The half's rows of the pieces before have left.  Waited for also where this piece has nothing for the half: what was noted of
+                        // the last tiles (bars.odd) is read on the way out, and the notes come round after eight tiles
+                        if (ok && t == p.first && rounds[i] > 0) ok = wait(&bars.ofree[i], (uint32_t)(rounds[i] - 1) & 1u);
                         if (!ok || t >= p.end[i]) continue;
-                        if (t == p.first && rounds[i] > 0) ok = wait(&bars.ofree[i], (uint32_t)(rounds[i] - 1) & 1u);
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {            // weights of positions 0-63, then the others
                             ok = ok && wait(&bars.pready[i][j], done[i] & 1u);

@@ -116,3 +116,24 @@ def test_a_nan_of_hardly_any_weight(b, kind, dtype, rows, heads):
     c.fill()
     got = attend(b, c, [torch.ones(rows, heads, 128)])
     assert np.isnan(got[:rows]).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_blocks_of_two_halves_before_blocks_of_one(b, kind, dim):
+    """A CTA's run of many short items: what is not a number in the last tiles of a block of 200 rows reaches its second half's rows, however long
+    the three blocks of 36 rows behind it, which have no second half, run ahead."""
+    rows, kv = (200, 36, 36, 36) * 100, tuple(n for i in range(100) for n in ((7 * i) % 130, 90, 0, (5 * i) % 220))
+    c = pp.Case(b, rows, kv, 1, dim, 16, kind, BF16, seed=dim)
+    for s in range(0, 400, 4):
+        n = kv[s]
+        c.vals[s][n + 150, 0, 5] = float("nan")
+        if kind == "bf16":
+            c.vals[s][n + 199, 0, dim - 1], c.vals[s][n + 130, 0, 8] = float("inf"), -float("inf")
+    c.fill()
+    g = torch.Generator().manual_seed(8)
+    q = [torch.randn(r, 1, dim, generator=g) for r in rows]
+    got = attend(b, c, q)
+    for s in range(0, 400, 4):
+        mine = got[c.start[s]:c.start[s + 1], 0, 5]
+        assert not np.isnan(mine[:150]).any() and np.isnan(mine[150:]).all()
