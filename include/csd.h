@@ -336,7 +336,7 @@ csd_status csd_paged_read(const csd_kv_pool* pool, const csd_paged_batch* batch,
 /* Attention of the batch's rows over the cache that already holds their keys (csd_paged_append first):
  * out_r = sum_j softmax_j(scale * q_r . k_j) v_j over the positions j that the row sees: the kv_len before the chunk and,
  * of the chunk itself, its rows up to its own or, with tree_mask_dev [total_rows], the rows whose bit is set (bit j: row j
- * of the same sequence's chunk; max_rows <= 64).  A row that sees nothing is 0.  q_dev [total_rows, n_heads * d_head], rows ldq
+ * of the same sequence's chunk, bits behind its rows are nobody; max_rows <= 64).  A row that sees nothing is 0.  q_dev [total_rows, n_heads * d_head], rows ldq
  * elements apart, out_dev likewise with ldo (multiples of 8; 16-byte aligned; out may not overlap q).  n_heads is a multiple of
  * the pool's kv heads, at most 64 times as many; query head h reads kv head h / (n_heads / n_kv_heads).  Scores, softmax and sums are fp32; bf16 rows enter the products as they are
  * and their weights as bf16; fp32 rows and weights as three bf16 terms each (rows over 8-bit keys as two fp16 terms, 22 bits).

@@ -64,9 +64,10 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedView& w, int s) {
     return q;
 }
 
-// Rotary position of row i of a chunk: behind its ancestors, which are the rows of its mask other than itself; without masks all rows before it.
-__device__ __forceinline__ int rope_position(const PagedView& w, const RopeView& r, int kv, int i, const unsigned long long* mask) {
-    const int pos = kv + (mask ? __popcll(*mask & ~(1ull << (i & 63))) : i);
+// Rotary position of row i of a chunk of `rows`: behind its ancestors, which are the rows of its mask other than itself (bits behind the
+// chunk's rows are nobody); without masks all rows before it.
+__device__ __forceinline__ int rope_position(const PagedView& w, const RopeView& r, int kv, int i, int rows, const unsigned long long* mask) {
+    const int pos = kv + (mask ? __popcll(*mask & ~(1ull << (i & 63)) & (rows < 64 ? (1ull << rows) - 1 : ~0ull)) : i);
     if (pos >= r.positions) set_status(w.status, CSD_ERR_CAPACITY);
     return min(pos, r.positions - 1);
 }

@@ -18,8 +18,8 @@ struct RowsView {
     RopeView rope; const unsigned long long* tree;       // (append alone, fp32 rows: the model's keys are turned on their way)
 };
 
-// Sequence that row r of the batch belongs to, its lengths, and the row's position; false: to none.  Whole warps.
-__device__ __forceinline__ bool find_row(const PagedView& w, int r, int* seq, int* pos, int* row = nullptr) {
+// Sequence that row r of the batch belongs to, and the row's position (and its number in the chunk and the chunk's rows); false: to none.  Whole warps.
+__device__ __forceinline__ bool find_row(const PagedView& w, int r, int* seq, int* pos, int* row = nullptr, int* rows = nullptr) {
     const int lane = threadIdx.x & 31;
     int s = 0;
     for (int b = 0; b < w.n_seqs; b += 32) {
@@ -31,7 +31,7 @@ __device__ __forceinline__ bool find_row(const PagedView& w, int r, int* seq, in
     if (s >= w.n_seqs) return false;
     const PagedSeq q = paged_seq(w, s);
     *seq = s; *pos = q.kv + r - q.start;
-    if (row) *row = r - q.start;
+    if (row) { *row = r - q.start; *rows = q.rows; }
     return r >= q.start && r - q.start < q.rows;
 }
 
@@ -95,9 +95,9 @@ paged_append_kernel(const PagedView w, const RowsView src, int split) {
         for (int b = 0; b < BATCH; ++b)
             if (h0 + b * next + p.head < w.heads) load8<ROWS16>(from + (size_t)(h0 + b * next) * DH * SIZE, x[b]);
         if (!looked) {                                               // (the first loads are under way)
-            int seq, pos, i;
-            if (!find_row(w, r, &seq, &pos, &i)) return;
-            if (!ROWS16 && src.rope.cos) turn = rope_position(w, src.rope, pos - i, i, src.tree ? src.tree + r : nullptr);
+            int seq, pos, i, rows;
+            if (!find_row(w, r, &seq, &pos, &i, &rows)) return;
+            if (!ROWS16 && src.rope.cos) turn = rope_position(w, src.rope, pos - i, i, rows, src.tree ? src.tree + r : nullptr);
             const int page = paged_page(w, seq, pos);
             if (page < 0) return;
             const size_t row = paged_row(w, page, p.head, pos);      // (of a head that may not exist: not written)

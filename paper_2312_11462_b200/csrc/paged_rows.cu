@@ -177,7 +177,7 @@ paged_rows_kernel(const PagedView w, const AttendArgs a) {
                             const float4 y = *reinterpret_cast<const float4*>(far), z = *reinterpret_cast<const float4*>(far + 4);
                             const float other[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
                             const int i = p / a.group;
-                            rope8(a.rope, rope_position(w, a.rope, at.q.kv, i, a.tree ? a.tree + at.q.start + i : nullptr), DH / 2, 8 * c, x, other);
+                            rope8(a.rope, rope_position(w, a.rope, at.q.kv, i, at.q.rows, a.tree ? a.tree + at.q.start + i : nullptr), DH / 2, 8 * c, x, other);
                         }
                     }
                 }
