@@ -290,7 +290,10 @@ csd_status csd_spec_verify(const void* target_probs_dev, int64_t ld_p, const voi
  *                max|x| <= 448 * 2^e over the row's finite entries (a power of two: scaling rounds
  *                nothing, and a stored value is exact in fp32 and bf16).  Infinities become
  *                +-448 * 2^e; at e = 120 the numbers end at 240
- *                (256 * 2^120 is none in fp32).  A row with a NaN gets the byte 255 and is NaN.
+ *                (256 * 2^120 is none in fp32).  A row with a NaN gets the byte 255 and is NaN.  All other rows
+ *                have bytes from 27 to 247 and no number that is NaN (0x7F, 0xFF): csd_paged_append sees to both,
+ *                who fills a pool in another way has to, for the attention does not look for such numbers (it
+ *                would cost 3 % behind few rows and 8 to 14 % in chunks).
  * A batch is a chunk of new rows for each sequence: rows row_start[s] .. row_start[s+1] - 1 of the
  * packed row arrays are sequence s at positions kv_len[s] .., kv_len[s] positions lie before them.
  * The arrays are on the device, so a captured call replays with other lengths.  Lengths of zero are
@@ -340,7 +343,11 @@ csd_status csd_paged_read(const csd_kv_pool* pool, const csd_paged_batch* batch,
  * elements apart, out_dev likewise with ldo (multiples of 8; 16-byte aligned; out may not overlap q).  n_heads is a multiple of
  * the pool's kv heads, at most 64 times as many; query head h reads kv head h / (n_heads / n_kv_heads).  Scores, softmax and sums are fp32; bf16 rows enter the products as they are
  * and their weights as bf16; fp32 rows and weights as three bf16 terms each (rows over 8-bit keys as two fp16 terms, 22 bits).
- * Infinities and NaN in the cache reach the rows that see them and no others.
+ * bf16 rows are divided by the sum of their rounded weights or, in chunks of more than 32 (row, query head) pairs a kv head, of the fp32 ones.
+ * Infinities and NaN in the cache reach the rows that see them and no others: a NaN in a key and a score of +inf make the row NaN, a
+ * NaN value that dimension of the row, an infinite value makes it infinite (NaN, where its weight is below fp32's range); a score of -inf is no weight,
+ * and a row of such scores alone is 0.  An infinity in a query leaves its row NaN or 0.  Running maxima may lag by a factor of 2^16: cached numbers up to
+ * 2^80 never overflow the sums, whatever the length; scores have to stay in fp32's range.
  * The workspace has to be zero before its first call; every call leaves it ready for the next, of any shape.  Calls that may overlap
  * on the GPU need workspaces of their own. */
 size_t csd_paged_attention_workspace_bytes(const csd_kv_pool* pool, const csd_paged_batch* batch, int n_heads, int row_type);

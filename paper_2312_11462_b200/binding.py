@@ -405,7 +405,8 @@ def _law_stride(t: torch.Tensor) -> int:
 
 class KvPool:
     """A paged cache over the caller's tensors: k and v [n_pages, n_kv_heads, page_size, d_head], bfloat16, or
-    float8_e4m3fn with the exponents k_exp and v_exp [n_pages, n_kv_heads, page_size] uint8."""
+    float8_e4m3fn with the exponents k_exp and v_exp [n_pages, n_kv_heads, page_size] uint8.  Rows that something other than
+    csd_paged_append has written hold no NaN among their 8-bit numbers, unless their exponent is 255."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: Optional[torch.Tensor] = None, v_exp: Optional[torch.Tensor] = None):
         n, H, P, D = k.shape

@@ -137,3 +137,33 @@ def test_blocks_of_two_halves_before_blocks_of_one(b, kind, dim):
     for s in range(0, 400, 4):
         mine = got[c.start[s]:c.start[s + 1], 0, 5]
         assert not np.isnan(mine[:150]).any() and np.isnan(mine[150:]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_what_an_8_bit_row_may_hold(b, dtype):
+    """Whatever is appended, a row's byte is 27 to 247 and none of its numbers is NaN, or the byte is 255."""
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn(400, 3, 64, generator=g) * torch.exp2(torch.randint(-149, 128, (400, 3, 1), generator=g).float())
+    x[::7, 0, 5], x[::11, 1, 6], x[::13, 2, 7] = float("inf"), -float("inf"), float("nan")
+    x[5], x[6], x[7], x[8] = 0.0, torch.finfo(F32).max, 480.0, -torch.finfo(F32).max
+    c = pp.Case(b, (400,), (0,), 3, 64, 16, "e4m3", dtype, pad_rows=0)
+    c.keys, c.vals = [x.to(dtype)], [(-x).to(dtype)]
+    c.fill()
+    at = torch.arange(400)
+    page, slot = c.table[0, at // 16].long(), at % 16
+    for rows, exps, given in ((c.pool.k, c.pool.k_exp, c.keys[0]), (c.pool.v, c.pool.v_exp, c.vals[0])):
+        numbers, e = rows.view(torch.uint8).cpu()[page, :, slot].int(), exps.cpu()[page, :, slot].int()
+        odd = given.isnan().any(-1)
+        assert (e[odd] == 255).all() and ((e[~odd] >= 27) & (e[~odd] <= 247)).all() and ((numbers[~odd] & 0x7F) != 0x7F).all()
+    assert b.csd_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,kv", [(1, 0), (3, 40), (40, 985), (300, 20)])
+def test_rows_whose_every_score_is_no_weight(b, dtype, rows, kv):
+    """Scores of -inf alone: 0, like a row that sees nothing, whole or in parts."""
+    c = pp.Case(b, (rows,), (kv,), 1, 64, 16, "bf16", dtype, seed=kv)
+    c.keys[0][..., 3] = -float("inf")
+    c.fill()
+    out = b.csd_paged_attention(c.packed([torch.randn(rows, 2, 64).abs()]), c.pool, c.batch())
+    assert (out[:rows] == 0).all() and b.csd_device_status() == 0
