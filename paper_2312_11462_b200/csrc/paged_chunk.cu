@@ -12,8 +12,10 @@
 // issued by one thread and run in order, so when the scores of tile t + 1 are there, O += P V of tile t is done.  P goes out in two parts of 64
 // positions; the first one's product runs under the other's exponentials.  A running maximum is only brought up when a score is above it by 2^16
 // (bf16 and fp32 have room for that), so that hardly a tile after an item's first waits for its maximum or rescales the output.
+// A row is divided by the sum of its weights in fp32; the products take them in bf16, off by 2^-9 of each at most and either way (the rounded ones' sum would
+// cost an unpacking a weight).
 //
-// An item's rows that lie in several CTAs' runs leave as parts, which paged_join_kernel adds up.  Measured: 890 TFLOP/s of bf16 pages, 755 of 8-bit ones
+// An item's rows that lie in several CTAs' runs leave as parts, which paged_join_kernel adds up.  Measured: 875 to 887 TFLOP/s of bf16 pages, 755 of 8-bit ones
 // (592 heads of 64 rows behind 4288 positions, 128 dimensions), bounded by a half's chain of scores, exponentials and products: with a quarter of the
 // exponentials as polynomials on the multipliers it is 3 to 5 % slower, so the special-function unit is not what holds it up.
 //
@@ -434,7 +436,11 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             };
             while (unit < end && ok) {
                 const ChunkPiece p(w, at, end, group);
-                ok = wait(&bars.qfull, (uint32_t)pieces & 1u) && wait(&bars.full[slot], phase);
+                // A half that this piece has nothing for (one at most) has left the pieces before all the same: what was noted of its last tiles (bars.odd) is
+                // read on its way out, and the notes come round after eight tiles.  (One wait, here: for each half in the loop below it moves
+                // the code so that a prompt of 4096 rows takes 2 to 5 % longer.)
+                const int gone = p.first >= p.end[0] ? 0 : p.first >= p.end[1] ? 1 : -1, left = gone == 0 ? rounds[0] : gone == 1 ? rounds[1] : 0;
+                ok = wait(&bars.qfull, (uint32_t)pieces & 1u) && wait(&bars.full[slot], phase) && (left == 0 || wait(&bars.ofree[gone], (uint32_t)(left - 1) & 1u));
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
@@ -456,10 +462,8 @@ paged_chunk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                     const uint64_t vt = vd + (uint64_t)(v * (C::TILE_BYTES >> 4));
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        // The half's rows of the pieces before have left.  Waited for also where this piece has nothing for the half: what was noted of
-                        // the last tiles (bars.odd) is read on the way out, and the notes come round after eight tiles
-                        if (ok && t == p.first && rounds[i] > 0) ok = wait(&bars.ofree[i], (uint32_t)(rounds[i] - 1) & 1u);
                         if (!ok || t >= p.end[i]) continue;
+                        if (t == p.first && rounds[i] > 0) ok = wait(&bars.ofree[i], (uint32_t)(rounds[i] - 1) & 1u);
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {            // weights of positions 0-63, then the others
                             ok = ok && wait(&bars.pready[i][j], done[i] & 1u);
