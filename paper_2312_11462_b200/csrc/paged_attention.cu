@@ -19,12 +19,15 @@ static int packed_rows(const csd_paged_batch* batch, const csd_kv_pool* pool, in
 }
 
 // Which kernel takes bf16 rows.  Up to 32 pairs are one or two blocks of 16 of the rows kernel, which then reads the cache once; from 33 on it
-// reads it several times, and the chunk kernel's block of 256 once.  32 heads on 8 of 128 dimensions, us in the rows and the chunk kernel:
-//   pairs   1 sequence x 16000   16 x 4000    64 x 2000
-//    16         28    34          57   85     104  144
-//    32         38    35          74   85     145  144
-//    48         52    33         135   87     268  146
-//   128         74    34         240   87     506  148
+// reads it several times, and the chunk kernel's block of 256 once.  32 heads on 8, us in the rows and the chunk kernel:
+//             1 sequence x 16000         16 x 4000                64 x 2000
+//   pairs    bf16   8 bits  64 dims    bf16   8 bits  64 dims    bf16    8 bits   64 dims
+//    16     29 37   25 41   23 34     57 77   51 95   37 70    104 148   94 181   66 130
+//    32     39 37   35 41   27 34     74 77   78 96   52 70    139 148  148 180   93 130
+//    48     49 37   48 41   35 34    130 77  142 96   91 70    258 149  272 180  174 130
+//   128     72 38   73 42   49 34    231 78  254 96  157 71    490 151  524 182  326 131
+// The longest chunk decides for all sequences of a call: 500 rows of one and a row of each of 63 others behind 2000 positions take 256 and 185 us (8
+// bits: 280 and 222).
 static bool takes_chunks(int packed, int row_type) { return row_type == CSD_BF16 && packed > 32; }
 
 extern "C" size_t csd_paged_attention_workspace_bytes(const csd_kv_pool* pool, const csd_paged_batch* batch, int n_heads, int row_type) {

@@ -2,9 +2,10 @@
 //
 // What bounds it is the cache: each visible page is read once per block of 16 or 32 (row, query head) pairs.  A CTA has twelve
 // or eight warps, one CTA an SM.  A key tile is one or two groups of 16 positions a warp, a group always inside one page; each warp
-// stages its own keys and values with cp.async, several tiles ahead, across the ends of items, and never waits for another warp until an item ends: it keeps
-// its own running maximum, sum and output, which the CTA's warps add up through shared memory.  An SM has 96 to 128 KB in flight that
-// way, twice what the memory's latency asks for.  Measured: bf16 rows of 128 at 6.5 TB/s, the copy rate; 8-bit ones at 4.6 (widening them).
+// stages its own keys and values with cp.async, across the ends of items, one tile ahead where twelve warps have tiles of 8 KB each and two to four elsewhere,
+// and never waits for another warp until an item ends: it keeps its own running maximum, sum and output, which the CTA's warps add up through shared memory.
+// An SM has 96 to 146 KB in flight that way (fp32 rows of 64 over 8 bits, more than 16 of them: 65), up to three times what the memory's latency asks for.
+// Measured: bf16 rows of 128 at 6.5 TB/s, the copy rate; 8-bit ones at 4.5 (issuing in 59 % of the cycles, most of it to widen them).
 //
 // Scores and outputs are mma.sync products (m16n8k16): at 16 rows a tile's products take a sixth of its loading time, and the
 // operands' layout leaves the scores' accumulators as the operands of the second product.  Rows in bf16 enter as they are, their weights as

@@ -6,8 +6,8 @@
 // contiguous piece of the law, the warps' sums go to all CTAs through distributed shared memory, and the warp whose piece holds
 // the target goes through it once more (from L2): lanes' stretches, then the stretch.  No workspace, one launch.
 //
-// What bounds it: many rows, the laws' bytes (256 rows of 128256 fp32 entries, most with a refused draft: 47.5 us, 75 % of the copy rate); one row, the
-// chain of tests, sums, exchange and second look (32000 entries 6.3 us).
+// What bounds it: many rows, the laws' bytes (256 rows of 128256 fp32 entries, most with a refused draft: 46 us, 77 % of the copy rate); one row, the
+// chain of tests, sums, exchange and second look (32000 entries 6.0 us).
 #include "tc_common.cuh"
 
 namespace csd {
