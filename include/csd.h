@@ -346,7 +346,7 @@ csd_status csd_paged_read(const csd_kv_pool* pool, const csd_paged_batch* batch,
  * bf16 rows are divided by the sum of their rounded weights or, in chunks of more than 32 (row, query head) pairs a kv head, of the fp32 ones.
  * Infinities and NaN in the cache reach the rows that see them and no others: a NaN in a key and a score of +inf make the row NaN, a
  * NaN value that dimension of the row, an infinite value makes it infinite (NaN, where its weight is below fp32's range); a score of -inf is no weight,
- * and a row of such scores alone is 0.  An infinity in a query leaves its row NaN or 0.  Running maxima may lag by a factor of 2^16: cached numbers up to
+ * and a row of such scores alone over finite values is 0.  An infinity in a query leaves its row NaN or 0.  Running maxima may lag by a factor of 2^16: cached numbers up to
  * 2^80 never overflow the sums, whatever the length; scores have to stay in fp32's range.
  * The workspace has to be zero before its first call; every call leaves it ready for the next, of any shape.  Calls that may overlap
  * on the GPU need workspaces of their own. */

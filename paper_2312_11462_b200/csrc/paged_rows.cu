@@ -448,8 +448,11 @@ paged_rows_kernel(const PagedView w, const AttendArgs a) {
                                     x = (k & ~6) == 8 * g + 1 ? uneven : x;
                                 }
                                 x = __shfl_sync(0xffffffffu, x, from);
-                                if (x == -INFINITY) continue;            // (not seen)
-                                const float weight = ex2(x - m[mt][hr]);
+                                // not seen, or a score of -inf: no weight, but what it sees that is not finite counts
+                                const int t1 = t0 + k, back = t1 - at.q.kv;
+                                const bool sees = t1 < lim[mt][hr] || (back >= 0 && back < 64 && t1 < at.seen && (bits[mt][hr] >> back & 1));
+                                if (x == -INFINITY && (!sees || (gone >> (k >> 4) & 1))) continue;
+                                const float weight = ex2(x - (m[mt][hr] == -INFINITY ? 0.f : m[mt][hr]));
 #pragma unroll
                                 for (int t = 0; t < DH / 8; ++t)
 #pragma unroll

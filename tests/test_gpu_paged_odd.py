@@ -167,3 +167,18 @@ def test_rows_whose_every_score_is_no_weight(b, dtype, rows, kv):
     c.fill()
     out = b.csd_paged_attention(c.packed([torch.randn(rows, 2, 64).abs()]), c.pool, c.batch())
     assert (out[:rows] == 0).all() and b.csd_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("rows,kv,heads,tree", [((1, 3), (40, 700), 2, False), ((7, 5), (30, 0), 2, True), ((20,), (300,), 1, False), ((60, 40), (50, 985), 2, False)])
+def test_a_nan_behind_a_score_of_no_weight(b, dtype, dim, rows, kv, heads, tree):
+    """A position whose key gives -inf and whose value is NaN: every row that sees it is NaN there, in tiles that all rows see and in those that
+    some see, whole or in parts; the others are not."""
+    c = pp.Case(b, rows, kv, 1, dim, 16, "bf16", dtype, seed=dim)
+    for k, v in zip(c.keys, c.vals):
+        for at in (len(k) // 5, len(k) - 1 - len(k) // 20):
+            k[at, 0, 3], v[at, 0, 9] = -float("inf"), float("nan")
+    c.fill()
+    g = torch.Generator().manual_seed(2)
+    attend(b, c, [torch.randn(r, heads, dim, generator=g).abs() for r in rows], pp.trees(rows, 4) if tree else None)
